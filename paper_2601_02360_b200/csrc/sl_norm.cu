@@ -373,6 +373,7 @@ __global__ void __launch_bounds__(kMaxThreads) norm_block_kernel(const NormArgs 
     const bool in = r < a.n;
     x.mask(c);
     if (a.b) b.mask(c);
+    if (a.g) g.mask(c);                                    // a NaN beside the row would outlast the zeros of x and b
     float h[K][E];
     float rp = a.alpha;                                    // factor of u: rms(b), with alpha in w_post, or alpha
     if (a.w_post) {
@@ -485,6 +486,7 @@ __global__ void __maxnreg__(128) norm_block_grad_kernel(const NormGradArgs a, co
     if (a.dh) dh.mask(c);
     if (a.dy) dy.mask(c);
     if (a.b) b.mask(c);
+    if (a.g) g.mask(c);
     float z[K][E];
     float s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
