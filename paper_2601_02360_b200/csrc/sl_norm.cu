@@ -17,6 +17,7 @@
 // at the same place: a thread's columns, its weights and its sums stay the same from row to row, and only the pieces
 // that hold a row's two ends go element by element.
 #include "sl_inner.cuh"
+#include "sl_norm_rows.cuh"
 
 namespace sl {
 namespace {
@@ -24,19 +25,6 @@ namespace {
 constexpr int kMaxThreads = 320;   // of a CTA
 constexpr int kMaxWarps = 40;       // of a row: a CTA of 10, or 8 CTAs of 5 warps
 enum Group { kLanes, kCta, kCluster };     // what shares a row
-
-// the columns of a thread: K pieces of E, the first of them `lead` columns before the row where rows are shifted
-template <int E, int K, bool SHIFT>
-struct Columns {
-  uint32_t first, step, parts, d, lead;
-  __device__ __forceinline__ uint32_t part(int k) const { return first + k * step; }
-  __device__ __forceinline__ bool any(int k) const { return part(k) < parts; }
-  // where a thread without a k-th piece loads, so that no load needs a condition
-  __device__ __forceinline__ int safe(int k) const { return any(k) ? col(k) : -(SHIFT ? (int)lead : 0); }
-  __device__ __forceinline__ int col(int k) const { return (int)(part(k) * E) - (SHIFT ? (int)lead : 0); }
-  __device__ __forceinline__ bool whole(int k) const { return !SHIFT || (col(k) >= 0 && col(k) + E <= (int)d); }
-  __device__ __forceinline__ bool has(int k, int e) const { return !SHIFT || (uint32_t)(col(k) + e) < d; }
-};
 
 // What a thread holds of a row, as it is stored; a piece that it does not have holds something else.  Nothing here looks at
 // what it loaded before mask(), so that the loads of a row's arrays are all on their way together.
@@ -49,15 +37,15 @@ struct Piece {
     if constexpr (sizeof(T) == 4) return __float_as_uint(__ldcs(reinterpret_cast<const float*>(p)));
     else return (uint32_t)__ldcs(reinterpret_cast<const uint16_t*>(p));
   }
-  // last: no row comes behind this one, so that a vector may not reach past its end
+  // near_end: too little comes behind this row for a vector that reaches past its end
   template <bool SHIFT>
-  __device__ __forceinline__ void load(const T* row, const Columns<E, K, SHIFT>& c, bool last) {
+  __device__ __forceinline__ void load(const T* row, const Columns<E, K, SHIFT>& c, bool near_end) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const T* p = row + c.safe(k);
       if constexpr (E == 1) {
         w[k][0] = bits(p);
-      } else if (SHIFT && last && (!c.any(k) || !c.whole(k))) {
+      } else if (!c.by_vector(k, near_end)) {
 #pragma unroll
         for (int i = 0; i < W; ++i) w[k][i] = 0;
 #pragma unroll
@@ -332,17 +320,6 @@ struct Rows {
     step = (uint64_t)(groups / l.period) * per * l.period;
   }
 };
-template <int E, int K, bool SHIFT>
-__device__ __forceinline__ Columns<E, K, SHIFT> columns_of(uint64_t row, uint32_t lane, uint32_t lanes, uint32_t d) {
-  Columns<E, K, SHIFT> c;
-  c.first = lane;
-  c.step = lanes;
-  c.d = d;
-  c.lead = SHIFT ? (uint32_t)(row * d % E) : 0;
-  c.parts = (d + c.lead + E - 1) / E;
-  return c;
-}
-
 template <class RT, class AT, int E, int K, Group G, bool SHIFT>
 __global__ void __launch_bounds__(kMaxThreads) norm_block_kernel(const NormArgs a, const Launch l) {
   extern __shared__ __align__(16) float weights[];
@@ -355,10 +332,10 @@ __global__ void __launch_bounds__(kMaxThreads) norm_block_kernel(const NormArgs 
   Piece<AT, E, K> b, g;
   auto load = [&](uint64_t r) {
     if (r >= a.n) return;
-    const bool last = r + 1 == a.n;
-    x.load(static_cast<const RT*>(a.x) + r * a.d, c, last);
-    if (a.b) b.load(static_cast<const AT*>(a.b) + r * a.ldb, c, last);
-    if (a.g) g.load(static_cast<const AT*>(a.g) + r * a.ldg, c, last);
+    const bool near_end = SHIFT && near_array_end(r, a.n, a.d);
+    x.load(static_cast<const RT*>(a.x) + r * a.d, c, near_end);
+    if (a.b) b.load(static_cast<const AT*>(a.b) + r * a.ldb, c, near_end);
+    if (a.g) g.load(static_cast<const AT*>(a.g) + r * a.ldg, c, near_end);
   };
   uint64_t r = rw.row;
   load(r);
@@ -459,15 +436,15 @@ __global__ void __maxnreg__(128) norm_block_grad_kernel(const NormGradArgs a, co
   float rh = 0.0f, rp = 1.0f;
   auto load = [&](uint64_t r) {
     if (r >= a.n) return;
-    const bool last = r + 1 == a.n;
-    h.load(static_cast<const RT*>(a.h) + r * a.d, c, last);
-    if (a.dh) dh.load(static_cast<const RT*>(a.dh) + r * a.d, c, last);
+    const bool near_end = SHIFT && near_array_end(r, a.n, a.d);
+    h.load(static_cast<const RT*>(a.h) + r * a.d, c, near_end);
+    if (a.dh) dh.load(static_cast<const RT*>(a.dh) + r * a.d, c, near_end);
     if (a.dy) {
-      dy.load(static_cast<const AT*>(a.dy) + r * a.d, c, last);
+      dy.load(static_cast<const AT*>(a.dy) + r * a.d, c, near_end);
       rh = __ldg(a.r_pre + r);
     }
-    if (a.b) b.load(static_cast<const AT*>(a.b) + r * a.ldb, c, last);
-    if (a.g) g.load(static_cast<const AT*>(a.g) + r * a.ldg, c, last);
+    if (a.b) b.load(static_cast<const AT*>(a.b) + r * a.ldb, c, near_end);
+    if (a.g) g.load(static_cast<const AT*>(a.g) + r * a.ldg, c, near_end);
     if (a.w_post) rp = __ldg(a.r_post + r);
   };
   uint64_t r = rw.row;

@@ -5,8 +5,9 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import inner as oi
 from paper_2601_02360_b200 import api
-from test_norm_block_gpu import ALPHA, DT, EPS, TYPES, _cuda, _inputs, _q
+from test_norm_block_gpu import ALPHA, DT, EPS, TYPES, U, _bounds, _check_forward, _cuda, _f64, _half_ulp, _inputs, _q
 
 pytestmark = pytest.mark.gpu
 NAN = float("nan")
@@ -60,3 +61,32 @@ def test_what_lies_between_rows_does_not_count(d, gap, res, act):
     for k in one:
         assert np.isfinite(two[k]).all() and np.array_equal(one[k], two[k]), k
     assert all(np.array_equal(p, q) for p, q in zip(w1, w2))
+
+
+@pytest.mark.parametrize("n,d", [(2, 1), (3, 1), (9, 1), (4, 2), (5, 3), (3, 4), (7, 5), (9, 6), (2, 7), (40, 3)])
+@pytest.mark.parametrize("res,act", TYPES)
+def test_narrow_rows(n, d, res, act):
+    """rows narrower than a vector against the checker; the arrays end where their last row does, with NaN behind them"""
+    x, b, g, wp, wn = _inputs(n, d, "all", res, act, "f")
+
+    def tight(a, t):
+        w = torch.full((n * d + 64,), NAN, dtype=DT[t], device="cuda")
+        w[:n * d] = torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).cuda().reshape(-1)
+        return w[:n * d].view(n, d)
+    h, y = tight(np.zeros((n, d)), res), tight(np.zeros((n, d)), act)
+    rp, rn = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    ins = [tight(x, res), tight(b, act), tight(g, act), _cuda(wp), _cuda(wn)]
+    api.sl_norm_block(*ins, n, d, ALPHA, EPS, h, y, rp, rn)
+    _check_forward([t.float().cpu().numpy() for t in (h, y, rp, rn)], x, b, g, wp, wn, res, act)
+    r = np.random.default_rng(n)
+    dh, dy = _q(r.standard_normal((n, d)), res), _q(r.standard_normal((n, d)), act)
+    outs = dict(dx=tight(dh, res), db=tight(dh, act), dg=tight(dh, act), dw_post=torch.empty(d, device="cuda"), dw_pre=torch.empty(d, device="cuda"))
+    ws = torch.empty(api.sl_norm_block_grad_workspace(n, d), dtype=torch.uint8, device="cuda")
+    api.sl_norm_block_grad(tight(dh, res), tight(dy, act), h, *ins[1:], rp, rn, n, d, ALPHA, *outs.values(), False, ws)
+    f = _f64(dh, dy, h.float().cpu().numpy(), b, g, wp, wn, rp.cpu().numpy(), rn.cpu().numpy())
+    want, mags = oi.norm_block_grad(*f, float(np.float32(ALPHA))), _bounds(*f, ALPHA)
+    gate = 2.4 * np.abs(f[4])
+    for k, t in outs.items():                              # the bounds of the wider shapes
+        steps = n + 160 + gate.max() if k.startswith("dw") else 160 + np.maximum(gate, np.max(gate, 1, keepdims=True))
+        tol = steps * U * mags[k] + (0.0 if k.startswith("dw") else _half_ulp(want[k], res if k == "dx" else act))
+        assert np.all(np.abs(t.float().cpu().numpy() - want[k]) <= tol + 1e-37), k
