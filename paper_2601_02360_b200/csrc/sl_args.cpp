@@ -32,6 +32,22 @@ const char* type_names(int mask) {
   }
 }
 
+// Accessors of a tensor may throw (data_ptr() and stride() of tensors without storage or strides): a Python error, since
+// no C++ exception may leave a C function.
+template <class F>
+PyObject* guarded(F&& f) {
+  try {
+    return f();
+  } catch (const c10::Error& e) {
+    PyErr_SetString(PyExc_ValueError, e.what_without_backtrace());
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_ValueError, e.what());
+  } catch (...) {
+    PyErr_SetString(PyExc_ValueError, "unknown C++ exception");
+  }
+  return nullptr;
+}
+
 PyObject* refuse(PyObject* name, PyObject* t, const char* what, long long a, long long b, int mask) {
   PyErr_Format(PyExc_ValueError, what, name, type_names(mask), a, b, t == nullptr ? Py_None : (PyObject*)Py_TYPE(t));
   return nullptr;
@@ -48,13 +64,15 @@ PyObject* ptr(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const long long numel = PyLong_AsLongLong(args[2]);
   const long mask = PyLong_AsLong(args[3]);
   if (PyErr_Occurred()) return nullptr;
-  if (THPVariable_Check(o)) {
-    const at::Tensor& t = THPVariable_Unpack(o);
-    if ((type_bit(t.scalar_type()) & mask) && t.is_cuda() && t.numel() >= numel && t.is_contiguous())
-      return PyLong_FromUnsignedLongLong((unsigned long long)(uintptr_t)t.data_ptr());
-  }
-  return refuse(args[1], o, "%U: expected a contiguous CUDA tensor of %s with at least %lld elements (got %lld, %R)", numel,
-                THPVariable_Check(o) ? (long long)THPVariable_Unpack(o).numel() : -1, (int)mask);
+  return guarded([&]() -> PyObject* {
+    if (THPVariable_Check(o)) {
+      const at::Tensor& t = THPVariable_Unpack(o);
+      if ((type_bit(t.scalar_type()) & mask) && t.is_cuda() && t.numel() >= numel && t.is_contiguous())
+        return PyLong_FromUnsignedLongLong((unsigned long long)(uintptr_t)t.data_ptr());
+    }
+    return refuse(args[1], o, "%U: expected a contiguous CUDA tensor of %s with at least %lld elements (got %lld, %R)", numel,
+                  THPVariable_Check(o) ? (long long)THPVariable_Unpack(o).numel() : -1, (int)mask);
+  });
 }
 
 // rows(matrix or None, name, n, d, type mask) -> (device pointer, elements between rows); (0, d) for None
@@ -68,18 +86,20 @@ PyObject* rows(PyObject*, PyObject* const* args, Py_ssize_t k) {
   const long mask = PyLong_AsLong(args[4]);
   if (PyErr_Occurred()) return nullptr;
   if (o == Py_None) return Py_BuildValue("(iL)", 0, d);
-  if (THPVariable_Check(o)) {
-    const at::Tensor& t = THPVariable_Unpack(o);
-    if ((type_bit(t.scalar_type()) & mask) && t.is_cuda() && t.dim() == 2 && t.size(0) >= n && t.size(1) == d &&
-        (d == 1 || t.stride(1) == 1) && (n <= 1 || t.stride(0) >= d))
-      return Py_BuildValue("(KL)", (unsigned long long)(uintptr_t)t.data_ptr(), n > 1 ? (long long)t.stride(0) : d);
-  }
-  return refuse(args[1], o, "%U: expected a CUDA matrix of %s with dense, evenly spaced rows, %lld x %lld (got %R)", n, d, (int)mask);
+  return guarded([&]() -> PyObject* {
+    if (THPVariable_Check(o)) {
+      const at::Tensor& t = THPVariable_Unpack(o);
+      if ((type_bit(t.scalar_type()) & mask) && t.is_cuda() && t.dim() == 2 && t.size(0) >= n && t.size(1) == d &&
+          (d == 1 || t.stride(1) == 1) && (n <= 1 || t.stride(0) >= d))
+        return Py_BuildValue("(KL)", (unsigned long long)(uintptr_t)t.data_ptr(), n > 1 ? (long long)t.stride(0) : d);
+    }
+    return refuse(args[1], o, "%U: expected a CUDA matrix of %s with dense, evenly spaced rows, %lld x %lld (got %R)", n, d, (int)mask);
+  });
 }
 
 // type(tensor) -> bit of its type mask, 0 if unknown
 PyObject* type(PyObject*, PyObject* o) {
-  return PyLong_FromLong(THPVariable_Check(o) ? type_bit(THPVariable_Unpack(o).scalar_type()) : 0);
+  return guarded([&]() -> PyObject* { return PyLong_FromLong(THPVariable_Check(o) ? type_bit(THPVariable_Unpack(o).scalar_type()) : 0); });
 }
 
 PyMethodDef methods[] = {
