@@ -53,6 +53,10 @@ PyObject* refuse(PyObject* name, PyObject* t, const char* what, long long a, lon
   return nullptr;
 }
 
+// A tensor of which nothing will be read may have no memory; any other without memory (a fake tensor, a wrapper around other
+// tensors) is refused: its null pointer would say that an optional argument is absent.
+bool backed(const void* p, long long numel) { return p != nullptr || numel <= 0; }
+
 // ptr(tensor or None, name, numel, type mask) -> device pointer (0 for None)
 PyObject* ptr(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != 4) {
@@ -67,8 +71,10 @@ PyObject* ptr(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
     if (THPVariable_Check(o)) {
       const at::Tensor& t = THPVariable_Unpack(o);
-      if ((type_bit(t.scalar_type()) & mask) && t.is_cuda() && t.numel() >= numel && t.is_contiguous())
-        return PyLong_FromUnsignedLongLong((unsigned long long)(uintptr_t)t.data_ptr());
+      if ((type_bit(t.scalar_type()) & mask) && t.is_cuda() && t.numel() >= numel && t.is_contiguous()) {
+        const void* p = t.data_ptr();
+        if (backed(p, numel)) return PyLong_FromUnsignedLongLong((unsigned long long)(uintptr_t)p);
+      }
     }
     return refuse(args[1], o, "%U: expected a contiguous CUDA tensor of %s with at least %lld elements (got %lld, %R)", numel,
                   THPVariable_Check(o) ? (long long)THPVariable_Unpack(o).numel() : -1, (int)mask);
@@ -90,8 +96,10 @@ PyObject* rows(PyObject*, PyObject* const* args, Py_ssize_t k) {
     if (THPVariable_Check(o)) {
       const at::Tensor& t = THPVariable_Unpack(o);
       if ((type_bit(t.scalar_type()) & mask) && t.is_cuda() && t.dim() == 2 && t.size(0) >= n && t.size(1) == d &&
-          (d == 1 || t.stride(1) == 1) && (n <= 1 || t.stride(0) >= d))
-        return Py_BuildValue("(KL)", (unsigned long long)(uintptr_t)t.data_ptr(), n > 1 ? (long long)t.stride(0) : d);
+          (d == 1 || t.stride(1) == 1) && (n <= 1 || t.stride(0) >= d)) {
+        const void* p = t.data_ptr();
+        if (backed(p, n * d)) return Py_BuildValue("(KL)", (unsigned long long)(uintptr_t)p, n > 1 ? (long long)t.stride(0) : d);
+      }
     }
     return refuse(args[1], o, "%U: expected a CUDA matrix of %s with dense, evenly spaced rows, %lld x %lld (got %R)", n, d, (int)mask);
   });

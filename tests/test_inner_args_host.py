@@ -41,3 +41,14 @@ BOTH = "(refused(lambda: c.ptr(t, 'x', 4, 1)), refused(lambda: c.rows(t, 'x', 2,
 def test_accessors_that_throw_raise(how):
     out = _child("with FakeTensorMode(allow_non_fake_inputs=True):\n    " + how % BOTH)
     assert out.count("refused:") == 2
+
+
+def test_a_tensor_without_memory_is_not_an_absent_one():
+    out = _child("""
+with FakeTensorMode(allow_non_fake_inputs=True):
+    t = torch.empty(2, 2, device='cuda')
+    refused(lambda: c.ptr(t, 'x', 4, 1))
+    refused(lambda: c.rows(t, 'x', 2, 2, 1))
+    assert c.ptr(t[:0], 'x', 0, 1) == 0 and c.ptr(None, 'x', 4, 1) == 0
+""")
+    assert out.count("refused:") == 2
