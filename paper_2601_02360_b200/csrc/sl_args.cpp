@@ -57,6 +57,9 @@ PyObject* refuse(PyObject* name, PyObject* t, const char* what, long long a, lon
 // tensors) is refused: its null pointer would say that an optional argument is absent.
 bool backed(const void* p, long long numel) { return p != nullptr || numel <= 0; }
 
+// what is in memory is the tensor: not so for a view that is negated when it is read (the imaginary part of a conjugate)
+bool plain(const at::Tensor& t) { return !t.is_neg(); }
+
 // ptr(tensor or None, name, numel, type mask) -> device pointer (0 for None)
 PyObject* ptr(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != 4) {
@@ -71,7 +74,7 @@ PyObject* ptr(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
     if (THPVariable_Check(o)) {
       const at::Tensor& t = THPVariable_Unpack(o);
-      if ((type_bit(t.scalar_type()) & mask) && t.is_cuda() && t.numel() >= numel && t.is_contiguous()) {
+      if ((type_bit(t.scalar_type()) & mask) && t.is_cuda() && plain(t) && t.numel() >= numel && t.is_contiguous()) {
         const void* p = t.data_ptr();
         if (backed(p, numel)) return PyLong_FromUnsignedLongLong((unsigned long long)(uintptr_t)p);
       }
@@ -95,7 +98,7 @@ PyObject* rows(PyObject*, PyObject* const* args, Py_ssize_t k) {
   return guarded([&]() -> PyObject* {
     if (THPVariable_Check(o)) {
       const at::Tensor& t = THPVariable_Unpack(o);
-      if ((type_bit(t.scalar_type()) & mask) && t.is_cuda() && t.dim() == 2 && t.size(0) >= n && t.size(1) == d &&
+      if ((type_bit(t.scalar_type()) & mask) && t.is_cuda() && plain(t) && t.dim() == 2 && t.size(0) >= n && t.size(1) == d &&
           (d == 1 || t.stride(1) == 1) && (n <= 1 || t.stride(0) >= d)) {
         const void* p = t.data_ptr();
         if (backed(p, n * d)) return Py_BuildValue("(KL)", (unsigned long long)(uintptr_t)p, n > 1 ? (long long)t.stride(0) : d);

@@ -18,7 +18,7 @@ from . import api
 
 
 def _dense(t):
-    return None if t is None else t.contiguous()
+    return None if t is None else t.resolve_neg().contiguous()
 
 
 class _EmbedLookup(torch.autograd.Function):
@@ -27,7 +27,7 @@ class _EmbedLookup(torch.autograd.Function):
         V, d = T_S.shape
         n, L = ids.numel(), (pos.shape[0] if pos is not None else max(1, ids.shape[-1]))
         X = torch.empty(n, d, dtype=out_dtype or T_S.dtype, device=T_S.device)
-        ids = ids.contiguous()
+        ids = _dense(ids)
         api.sl_embed_lookup(ids, _dense(T_S), _dense(T_perp), _dense(pos), scale, n, L, V, d, X, flags)
         ctx.save_for_backward(ids)
         ctx.sizes = (n, L, V, d, scale, T_S.dtype, flags)
@@ -41,7 +41,7 @@ class _EmbedLookup(torch.autograd.Function):
         dT = torch.empty(V, d, dtype=dtype, device=dX.device)
         dpos = torch.empty(L, d, dtype=dtype, device=dX.device) if need_pos else None
         ws = torch.empty(api.sl_embed_grad_workspace(n, V, d), dtype=torch.uint8, device=dX.device)
-        api.sl_embed_grad(ids, dX.contiguous(), scale, n, L, V, d, dT, dpos, False, ws, flags)
+        api.sl_embed_grad(ids, _dense(dX), scale, n, L, V, d, dT, dpos, False, ws, flags)
         return None, (dT if need_s else None), (dT if need_p else None), dpos, None, None, None
 
 
@@ -56,7 +56,7 @@ class _NormBlock(torch.autograd.Function):
     def forward(ctx, x, b, g, w_post, w_pre, alpha, eps):
         d = x.shape[-1]
         n = x.numel() // d
-        x2 = x.reshape(n, d).contiguous()
+        x2 = _dense(x.reshape(n, d))
         rows = lambda t: None if t is None else _rows(t, n, d)  # noqa: E731
         b2, g2 = rows(b), rows(g)
         act = (b2 if b2 is not None else x2).dtype
@@ -76,7 +76,7 @@ class _NormBlock(torch.autograd.Function):
         n, d, alpha, shape = ctx.args
         if dh is None and dy is None:
             return (None,) * 7
-        dh, dy = (None if t is None else t.reshape(n, d).contiguous() for t in (dh, dy))
+        dh, dy = (None if t is None else _dense(t.reshape(n, d)) for t in (dh, dy))
         if dy is None:                    # nothing came back through the second norm
             zero_pre, w_pre, r_pre = (None if w_pre is None else torch.zeros_like(w_pre)), None, None
         dx = torch.empty_like(h)
@@ -95,6 +95,7 @@ class _NormBlock(torch.autograd.Function):
 
 def _rows(t, n: int, d: int):
     """t as n dense rows of d; columns of a wider matrix stay where they are."""
+    t = t.resolve_neg()
     v = t.view(n, d) if t.dim() != 2 and t.is_contiguous() else t
     return v if v.dim() == 2 and v.stride(1) == 1 and (n <= 1 or v.stride(0) >= d) else t.reshape(n, d).contiguous()
 
