@@ -22,16 +22,17 @@ def _dense(t):
 
 
 class _EmbedLookup(torch.autograd.Function):
+    """Dense arguments: ids [n], tables [V, d], positions [L, d]."""
+
     @staticmethod
-    def forward(ctx, ids, T_S, T_perp, pos, scale, flags, out_dtype):
+    def forward(ctx, ids, T_S, T_perp, pos, L, scale, flags, out_dtype):
         V, d = T_S.shape
-        n, L = ids.numel(), (pos.shape[0] if pos is not None else max(1, ids.shape[-1]))
+        n = ids.numel()
         X = torch.empty(n, d, dtype=out_dtype or T_S.dtype, device=T_S.device)
-        ids = _dense(ids)
-        api.sl_embed_lookup(ids, _dense(T_S), _dense(T_perp), _dense(pos), scale, n, L, V, d, X, flags)
+        api.sl_embed_lookup(ids, T_S, T_perp, pos, scale, n, L, V, d, X, flags)
         ctx.save_for_backward(ids)
         ctx.sizes = (n, L, V, d, scale, T_S.dtype, flags)
-        return X.view(*ids.shape, d)
+        return X
 
     @staticmethod
     def backward(ctx, dX):
@@ -42,68 +43,80 @@ class _EmbedLookup(torch.autograd.Function):
         dpos = torch.empty(L, d, dtype=dtype, device=dX.device) if need_pos else None
         ws = torch.empty(api.sl_embed_grad_workspace(n, V, d), dtype=torch.uint8, device=dX.device)
         api.sl_embed_grad(ids, _dense(dX), scale, n, L, V, d, dT, dpos, False, ws, flags)
-        return None, (dT if need_s else None), (dT if need_p else None), dpos, None, None, None
+        return None, (dT if need_s else None), (dT if need_p else None), dpos, None, None, None, None
 
 
 def embed_lookup(ids, T_S, T_perp=None, pos=None, scale: float = 1.0, flags=None, out_dtype=None):
     """scale (T_S[ids] + T_perp[ids]) + pos[t mod L] for int32 ids of any shape, [..., d]; token t is the t-th of the
     flattened ids, L the rows of pos.  Differentiable in T_S, T_perp and pos."""
-    return _EmbedLookup.apply(ids, T_S, T_perp, pos, float(scale), flags, out_dtype)
+    if T_S.dim() != 2 or (T_perp is not None and T_perp.shape != T_S.shape):
+        raise ValueError(f"T_S, T_perp: expected two matrices of one shape, got {list(T_S.shape)} and {None if T_perp is None else list(T_perp.shape)}")
+    if pos is not None and (pos.dim() != 2 or pos.shape[0] < 1 or pos.shape[1] != T_S.shape[1]):
+        raise ValueError(f"pos: expected rows of {T_S.shape[1]}, got {list(pos.shape)}")
+    L = pos.shape[0] if pos is not None else 1
+    X = _EmbedLookup.apply(_dense(ids.reshape(-1)), _dense(T_S), _dense(T_perp), _dense(pos), L, float(scale), flags, out_dtype)
+    return X.view(*ids.shape, T_S.shape[1])
 
 
 class _NormBlock(torch.autograd.Function):
+    """x dense [n, d]; b and g rows of d, evenly spaced; weights dense [d]."""
+
     @staticmethod
     def forward(ctx, x, b, g, w_post, w_pre, alpha, eps):
-        d = x.shape[-1]
-        n = x.numel() // d
-        x2 = _dense(x.reshape(n, d))
-        rows = lambda t: None if t is None else _rows(t, n, d)  # noqa: E731
-        b2, g2 = rows(b), rows(g)
-        act = (b2 if b2 is not None else x2).dtype
-        h = torch.empty_like(x2) if b2 is not None else None
+        n, d = x.shape
+        act = (b if b is not None else x).dtype
+        h = torch.empty_like(x) if b is not None else None
         y = torch.empty(n, d, dtype=act, device=x.device) if w_pre is not None else None
         stat = lambda w: None if w is None else torch.empty(n, dtype=torch.float32, device=x.device)  # noqa: E731
         r_post, r_pre = stat(w_post), stat(w_pre)
-        api.sl_norm_block(x2, b2, g2, _dense(w_post), _dense(w_pre), n, d, alpha, eps, h, y, r_post, r_pre)
-        ctx.save_for_backward(h if h is not None else x2, b2, g2, w_post, w_pre, r_post, r_pre)
-        ctx.args = (n, d, alpha, x.shape)
+        api.sl_norm_block(x, b, g, w_post, w_pre, n, d, alpha, eps, h, y, r_post, r_pre)
+        ctx.save_for_backward(h if h is not None else x, b, g, w_post, w_pre, r_post, r_pre)
+        ctx.args = (n, d, alpha)
         ctx.set_materialize_grads(False)
-        return (None if h is None else h.view(x.shape)), (None if y is None else y.view(x.shape))
+        return h, y
 
     @staticmethod
     def backward(ctx, dh, dy):
         h, b, g, w_post, w_pre, r_post, r_pre = ctx.saved_tensors
-        n, d, alpha, shape = ctx.args
+        n, d, alpha = ctx.args
         if dh is None and dy is None:
             return (None,) * 7
-        dh, dy = (None if t is None else _dense(t.reshape(n, d)) for t in (dh, dy))
+        dh, dy = _dense(dh), _dense(dy)
         if dy is None:                    # nothing came back through the second norm
             zero_pre, w_pre, r_pre = (None if w_pre is None else torch.zeros_like(w_pre)), None, None
         dx = torch.empty_like(h)
         like = lambda t: None if t is None else torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device)  # noqa: E731
         db, dg = like(b), like(g)
-        dw_post = None if w_post is None else torch.empty(d, dtype=w_post.dtype, device=h.device)
-        dw_pre = None if w_pre is None else torch.empty(d, dtype=w_pre.dtype, device=h.device)
+        dw_post, dw_pre = like(w_post), like(w_pre)
         ws = torch.empty(api.sl_norm_block_grad_workspace(n, d), dtype=torch.uint8, device=h.device)
-        api.sl_norm_block_grad(dh, dy, h, b, g, _dense(w_post), _dense(w_pre), r_post, r_pre, n, d, alpha, dx, db, dg, dw_post, dw_pre, False,
-                               ws)
+        api.sl_norm_block_grad(dh, dy, h, b, g, w_post, w_pre, r_post, r_pre, n, d, alpha, dx, db, dg, dw_post, dw_pre, False, ws)
         if dy is None:
             dw_pre = zero_pre
-        back = lambda t: None if t is None else t.reshape(shape)  # noqa: E731
-        return back(dx), back(db), back(dg), dw_post, dw_pre, None, None
+        return dx, db, dg, dw_post, dw_pre, None, None
 
 
-def _rows(t, n: int, d: int):
+def _rows(name: str, t, n: int, d: int):
     """t as n dense rows of d; columns of a wider matrix stay where they are."""
-    t = t.resolve_neg()
-    v = t.view(n, d) if t.dim() != 2 and t.is_contiguous() else t
-    return v if v.dim() == 2 and v.stride(1) == 1 and (n <= 1 or v.stride(0) >= d) else t.reshape(n, d).contiguous()
+    if t is None:
+        return None
+    if t.shape[-1:] != (d,) or t.numel() != n * d:
+        raise ValueError(f"{name}: expected {n} rows of {d}, got {list(t.shape)}")
+    v = t.resolve_neg().reshape(n, d)
+    return v if v.stride(1) == 1 and (n <= 1 or v.stride(0) >= d) else v.contiguous()
 
 
 def norm_block(x, b=None, g=None, w_post=None, w_pre=None, alpha: float = 1.0, eps: float = 1e-6):
     """(h, y): h = x + alpha sigmoid(g) norm(b) w_post and y = norm(h) w_pre, each term left out where its tensor is
-    None (no b: h is None and y = norm(x) w_pre; no w_pre: y is None).  Differentiable in every tensor."""
-    return _NormBlock.apply(x, b, g, w_post, w_pre, float(alpha), float(eps))
+    None (no b: h is None and y = norm(x) w_pre; no w_pre: y is None).  x, b and g: rows of one width in any shape, as many of
+    each; h and y have x's.  Differentiable in every tensor."""
+    d = x.shape[-1] if x.dim() else 0
+    if d < 1:
+        raise ValueError(f"x: expected rows, got {list(x.shape)}")
+    n = x.numel() // d
+    weight = lambda name, w: None if w is None else _rows(name, w, 1, d).reshape(d)  # noqa: E731
+    h, y = _NormBlock.apply(_dense(x.reshape(n, d)), _rows("b", b, n, d), _rows("g", g, n, d), weight("w_post", w_post),
+                            weight("w_pre", w_pre), float(alpha), float(eps))
+    return (None if h is None else h.view(x.shape)), (None if y is None else y.view(x.shape))
 
 
 class AdamW:

@@ -30,3 +30,52 @@ def test_views_that_are_negated_when_read():
         assert torch.equal(got, want)
     ids = torch.arange(n, dtype=torch.int32, device="cuda")
     assert torch.equal(inner.embed_lookup(ids, torch._neg_view(T)), -T)
+
+
+def test_operands_of_another_shape_than_x():
+    """the same rows in another shape give the same results, and every gradient has its tensor's shape"""
+    B, L, d = 3, 5, 40
+    g3 = [_randn(B, L, d, seed=i) for i in range(3)]
+    w = [_randn(d, seed=7), _randn(d, seed=8)]
+    wide = torch.cat([g3[1], g3[2]], -1)                  # b and g side by side
+
+    def run(x, b, g, wp, wn):
+        leaves = [t.detach().requires_grad_() for t in (x, b, g, wp, wn)]
+        h, y = inner.norm_block(*leaves, 0.5)
+        assert h.shape == x.shape and y.shape == x.shape
+        grads = torch.autograd.grad((h * 2).sum() + (y * y).sum(), leaves)
+        assert all(a.shape == t.shape for a, t in zip(grads, leaves))
+        return [h, y, *grads]
+    flat = lambda t: t.reshape(-1, d)  # noqa: E731
+    want = run(*map(flat, g3), *w)
+    for args in ((*g3, *w), (g3[0], flat(g3[1]), g3[2], *w), (flat(g3[0]), g3[1], flat(g3[2]), *w), (g3[0], wide[..., :d], wide[..., d:], *w),
+                 (*g3, w[0].view(1, d), w[1].view(1, 1, d)), (g3[0].transpose(0, 1).contiguous().transpose(0, 1), *g3[1:], *w)):
+        for a, b in zip(run(*args), want):
+            assert torch.equal(a.reshape(b.shape), b)
+
+
+def test_shapes_that_do_not_go_together_are_refused():
+    n, d = 6, 24
+    x, w = _randn(n, d), _randn(d, seed=1)
+    for b in (_randn(n + 1, d), _randn(n - 1, d), _randn(1, d), _randn(d, n), _randn(n, 2 * d), _randn(n * d)):
+        with pytest.raises(ValueError):
+            inner.norm_block(x, b, None, w, w)
+        with pytest.raises(ValueError):
+            inner.norm_block(x, x.clone(), b, w, w)
+    for bad in (_randn(2 * d), _randn(d - 1), _randn(d, 1), _randn(2, d)):
+        with pytest.raises(ValueError):
+            inner.norm_block(x, x.clone(), None, bad, w)
+        with pytest.raises(ValueError):
+            inner.norm_block(x, w_pre=bad)
+    with pytest.raises(ValueError):
+        inner.norm_block(torch.zeros((), device="cuda"), w_pre=w)
+    ids = torch.arange(4, dtype=torch.int32, device="cuda")
+    T = _randn(10, d)
+    for tp in (_randn(11, d), _randn(20, d // 2), _randn(10, d + 1)):
+        with pytest.raises(ValueError):
+            inner.embed_lookup(ids, T, tp)
+    for pos in (_randn(4, 2 * d), _randn(0, d), _randn(d), _randn(4, d - 1)):
+        with pytest.raises(ValueError):
+            inner.embed_lookup(ids, T, None, pos)
+    assert torch.equal(inner.embed_lookup(ids[3], T), T[3])                   # one id without a dimension
+    assert torch.equal(inner.embed_lookup(ids[3], T, None, T), T[3] + T[0])
