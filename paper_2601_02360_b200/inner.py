@@ -10,6 +10,7 @@ current stream; outputs and workspaces come from torch's allocator.
 """
 from __future__ import annotations
 
+import functools
 from typing import Optional, Sequence
 
 import torch
@@ -19,6 +20,33 @@ from . import api
 
 def _dense(t):
     return None if t is None else t.resolve_neg().contiguous()
+
+
+class _Once(torch.autograd.Function):
+    """Passes on gradients (behind the `k` tensors they depend on) into a graph that is being built: to differentiate them raises."""
+
+    @staticmethod
+    def forward(ctx, k, *tensors):
+        return tensors[k:]
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("embed_lookup and norm_block have no second derivative: no graph records the kernels of their gradients")
+
+
+def _once_differentiable(backward):
+    """Gradients from kernels would be constants to a graph of the backward pass (create_graph=True), and whatever passes through
+    them would be lost without an error.  They depend on the incoming gradients and on every saved tensor."""
+    @functools.wraps(backward)
+    def run(ctx, *grads):
+        with torch.no_grad():
+            out = backward(ctx, *grads)
+        if not torch.is_grad_enabled():
+            return out
+        depend = [t for t in (*grads, *ctx.saved_tensors) if t is not None and t.requires_grad]
+        given = iter(_Once.apply(len(depend), *depend, *(t for t in out if t is not None)))
+        return tuple(None if t is None else next(given) for t in out)
+    return run
 
 
 class _EmbedLookup(torch.autograd.Function):
@@ -35,6 +63,7 @@ class _EmbedLookup(torch.autograd.Function):
         return X
 
     @staticmethod
+    @_once_differentiable
     def backward(ctx, dX):
         (ids,) = ctx.saved_tensors
         n, L, V, d, scale, dtype, flags = ctx.sizes
@@ -48,7 +77,7 @@ class _EmbedLookup(torch.autograd.Function):
 
 def embed_lookup(ids, T_S, T_perp=None, pos=None, scale: float = 1.0, flags=None, out_dtype=None):
     """scale (T_S[ids] + T_perp[ids]) + pos[t mod L] for int32 ids of any shape, [..., d]; token t is the t-th of the
-    flattened ids, L the rows of pos.  Differentiable in T_S, T_perp and pos."""
+    flattened ids, L the rows of pos.  Differentiable in T_S, T_perp and pos; a second derivative raises RuntimeError."""
     if T_S.dim() != 2 or (T_perp is not None and T_perp.shape != T_S.shape):
         raise ValueError(f"T_S, T_perp: expected two matrices of one shape, got {list(T_S.shape)} and {None if T_perp is None else list(T_perp.shape)}")
     if pos is not None and (pos.dim() != 2 or pos.shape[0] < 1 or pos.shape[1] != T_S.shape[1]):
@@ -76,6 +105,7 @@ class _NormBlock(torch.autograd.Function):
         return h, y
 
     @staticmethod
+    @_once_differentiable
     def backward(ctx, dh, dy):
         h, b, g, w_post, w_pre, r_post, r_pre = ctx.saved_tensors
         n, d, alpha = ctx.args
@@ -108,7 +138,7 @@ def _rows(name: str, t, n: int, d: int):
 def norm_block(x, b=None, g=None, w_post=None, w_pre=None, alpha: float = 1.0, eps: float = 1e-6):
     """(h, y): h = x + alpha sigmoid(g) norm(b) w_post and y = norm(h) w_pre, each term left out where its tensor is
     None (no b: h is None and y = norm(x) w_pre; no w_pre: y is None).  x, b and g: rows of one width in any shape, as many of
-    each; h and y have x's.  Differentiable in every tensor."""
+    each; h and y have x's.  Differentiable in every tensor; a second derivative raises RuntimeError."""
     d = x.shape[-1] if x.dim() else 0
     if d < 1:
         raise ValueError(f"x: expected rows, got {list(x.shape)}")

@@ -79,3 +79,41 @@ def test_shapes_that_do_not_go_together_are_refused():
             inner.embed_lookup(ids, T, None, pos)
     assert torch.equal(inner.embed_lookup(ids[3], T), T[3])                   # one id without a dimension
     assert torch.equal(inner.embed_lookup(ids[3], T, None, T), T[3] + T[0])
+
+
+@pytest.mark.parametrize("incoming", ["constant", "of the graph"])
+@pytest.mark.parametrize("form", ["all", "first", "norm alone"])
+def test_a_second_derivative_of_the_norm_block_is_an_error(form, incoming):
+    n, d = 6, 40
+    x, b, g, w = (_randn(*s, seed=i).requires_grad_() for i, s in enumerate([(n, d), (n, d), (n, d), (d,)]))
+    up = torch.ones(n, d, device="cuda") if incoming == "constant" else x
+    a = {"all": (x, b, g, w, w, 0.5), "first": (x, None, None, None, w), "norm alone": (x, b, None, w, None)}[form]
+
+    def loss():
+        return sum((t * up).sum() for t in inner.norm_block(*a) if t is not None)
+    for leaf in (t for t in (x, b, w) if any(t is u for u in a)):
+        if form == "norm alone" and leaf is x:
+            continue                                      # h is linear in x
+        first, = torch.autograd.grad(loss(), leaf, create_graph=True)
+        with pytest.raises(RuntimeError, match="second derivative"):
+            torch.autograd.grad((first ** 2).sum() + (leaf ** 2).sum(), leaf)
+        with pytest.raises(RuntimeError, match="second derivative"):
+            first.sum().backward()
+    # a graph that is built and not used is no error, nor is one of other functions of the same tensors
+    built, = torch.autograd.grad(loss() + (x ** 3).sum(), x, create_graph=True)
+    plain, = torch.autograd.grad(loss() + (x ** 3).sum(), x)
+    assert torch.equal(built, plain)
+    two, = torch.autograd.grad((x ** 2).sum(), x, create_graph=True)
+    assert torch.equal(torch.autograd.grad(two.sum(), x)[0], torch.full_like(x, 2.0))
+
+
+def test_a_second_derivative_of_the_lookup():
+    d = 40
+    T, up = _randn(9, d, seed=5).requires_grad_(), _randn(6, d, seed=6).requires_grad_()
+    ids = torch.arange(6, dtype=torch.int32, device="cuda")
+    first, = torch.autograd.grad((inner.embed_lookup(ids, T) * up).sum(), T, create_graph=True)
+    with pytest.raises(RuntimeError, match="second derivative"):              # the gradient is linear in what comes in
+        torch.autograd.grad((first ** 2).sum(), up)
+    first, = torch.autograd.grad(inner.embed_lookup(ids, T).sum(), T, create_graph=True)
+    got, = torch.autograd.grad((first ** 2).sum() + (T ** 2).sum(), T)        # and does not depend on the table
+    assert torch.equal(got, 2 * T)
