@@ -288,7 +288,8 @@ int sl_adamw(void* theta, int theta_type, const void* grad, int grad_type, float
  * laws spend the codes where the moments are: near the top a code step is 1.6 % of m and of v, and v
  * reaches 2^-32 of the block's largest before it stops shrinking: v never becomes 0, which would make
  * the step m / eps.  theta moves by the moments BEFORE they are quantised, with the root and the quotient of
- * the move within 2^-20 of it (everything else is rounded as above).  A block with an Inf or NaN
+ * the move within 2^-20 of it where a 2^-41 <= eps <= 2^100 (a as above: from 1.4e-11 on at beta2 = 0.999), exact
+ * elsewhere (everything else is rounded as above).  A block with an Inf or NaN
  * gets the scale NaN, so that its moments read as NaN afterwards, and raises SL_FLAG_NONFINITE.
  *   m8 int8 [n_total], v8 uint8 [n_total]; m_scale, v_scale float [sl_adamw8_blocks(layout)]
  * Rounding to the nearest code loses changes of less than half a code step: 1 - beta should not be

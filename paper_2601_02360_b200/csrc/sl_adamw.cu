@@ -64,8 +64,9 @@ __device__ __forceinline__ float rcp_fast(float x) {       // 1 ulp
   return y;
 }
 // One element; `g` is the scaled gradient.  The file is compiled without contraction: each operation rounds once.
-// FAST: the root and the quotient of the move are within 2^-21 of it, which saves a fifth of the 8-bit form's
-// instructions (they and not bytes set its pace); the moments are the same to the bit.
+// FAST: the root (2^-23) and the quotient by a reciprocal (2^-23) leave the move within 2^-20 of the exact form's, which saves a
+// fifth of the 8-bit form's instructions (they and not bytes set its pace); the moments are the same to the bit.  Both flush
+// subnormal numbers, so not every eps allows it.
 template <bool FAST>
 __device__ __forceinline__ void adamw_element(const AdamwHyper& h, float keep, float g, float& m, float& v, float& theta) {
   m = h.beta1 * m + h.omb1 * g;
@@ -78,6 +79,11 @@ __device__ __forceinline__ void adamw_element(const AdamwHyper& h, float keep, f
     theta = theta * keep - h.c * __fdiv_rn(m, denom);
   }
 }
+
+// Whether FAST keeps its bound: a flushed v < 2^-126 takes less than 2^-63 a from denom, at most 2^-22 of it from this eps on
+// (1.4e-11 for a = 31.6, the first step at beta2 = 0.999; below, an eps that is subnormal itself would even give 0 * inf where
+// v = 0); and 1 / denom must not be subnormal.
+inline bool fast_move(const AdamwHyper& h) { return h.eps >= h.a * 0x1p-41f && h.eps <= 0x1p100f; }
 
 // the gradient's factor; false (with the flag raised): skip the step
 __device__ __forceinline__ bool gradient_scale(const float* p, uint32_t* flags, float& s) {
@@ -367,7 +373,7 @@ __device__ __forceinline__ bool quantise(const float (&m)[8], const float (&v)[8
 }
 
 // one block of the step, by a warp; false: some new moment is Inf or NaN
-template <class TH, class GR, Lanes M, int T>
+template <class TH, class GR, bool FAST, Lanes M, int T>
 __device__ __forceinline__ bool step_block(const AdamwArgs<T>& a, const Seg& sg, uint32_t g, uint32_t lane, float s) {
   const Lane<M> le(sg, lane);
   typename Lane<M>::template Held<TH> ht;
@@ -384,7 +390,7 @@ __device__ __forceinline__ bool step_block(const AdamwArgs<T>& a, const Seg& sg,
   le.take(hg, gr);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    adamw_element<true>(a.hy, sg.keep, s * gr[e], m[e], v[e], th[e]);
+    adamw_element<FAST>(a.hy, sg.keep, s * gr[e], m[e], v[e], th[e]);
     if (!le.has(e)) m[e] = v[e] = 0.0f;                    // behind the end of a short block
   }
   le.store(static_cast<TH*>(a.theta), th);
@@ -401,13 +407,13 @@ __device__ __forceinline__ bool step_block(const AdamwArgs<T>& a, const Seg& sg,
 }
 // the same out of line, so that the blocks that need more registers do not take them from the others (187 M elements: 679 us
 // with all three forms in line, 586 us with the whole blocks alone)
-template <class TH, class GR, Lanes M, int T>
+template <class TH, class GR, bool FAST, Lanes M, int T>
 __device__ __noinline__ bool step_block_apart(const AdamwArgs<T>& a, const Seg& sg, uint32_t g, uint32_t lane, float s) {
-  return step_block<TH, GR, M, T>(a, sg, g, lane, s);
+  return step_block<TH, GR, FAST, M, T>(a, sg, g, lane, s);
 }
 
 // 64 registers, so that four CTAs fit an SM
-template <class TH, class GR, int T>
+template <class TH, class GR, bool FAST, int T>
 __global__ void __maxnreg__(64) adamw8_kernel(const __grid_constant__ AdamwArgs<T> a) {
   float s;
   if (!gradient_scale(a.grad_scale, a.flags, s)) return;
@@ -418,9 +424,9 @@ __global__ void __maxnreg__(64) adamw8_kernel(const __grid_constant__ AdamwArgs<
   for (uint32_t g = blockIdx.x * (kThreads / 32) + threadIdx.x / 32; g < a.tb.n_blocks; g += warps) {
     const Seg sg = walk.at(g);
     const Lanes how = lanes_of(sg, a.aligned, n_total);
-    if (how == kWhole) bad |= !step_block<TH, GR, kWhole>(a, sg, g, lane, s);
-    else if (how == kShifted) bad |= !step_block_apart<TH, GR, kShifted>(a, sg, g, lane, s);
-    else bad |= !step_block_apart<TH, GR, kSingle>(a, sg, g, lane, s);
+    if (how == kWhole) bad |= !step_block<TH, GR, FAST, kWhole>(a, sg, g, lane, s);
+    else if (how == kShifted) bad |= !step_block_apart<TH, GR, FAST, kShifted>(a, sg, g, lane, s);
+    else bad |= !step_block_apart<TH, GR, FAST, kSingle>(a, sg, g, lane, s);
   }
   raise_nonfinite(bad, a.flags);
 }
@@ -500,7 +506,8 @@ cudaError_t launch_adamw8(const AdamwArgs<T>& a, int theta_type, int grad_type, 
   if (e != cudaSuccess) return e;
   return with_type(theta_type, [&](auto th) {
     return with_type(grad_type, [&](auto gr) {
-      adamw8_kernel<decltype(th), decltype(gr), T><<<grid, kThreads, 0, st>>>(a);
+      if (fast_move(a.hy)) adamw8_kernel<decltype(th), decltype(gr), true, T><<<grid, kThreads, 0, st>>>(a);
+      else adamw8_kernel<decltype(th), decltype(gr), false, T><<<grid, kThreads, 0, st>>>(a);
       return cudaPeekAtLastError();
     });
   });
