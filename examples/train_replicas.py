@@ -60,11 +60,11 @@ def loss_of(p, T_perp, pos, tokens, layers, ffn, alpha, flags):
     ids, target = tokens[:, :-1].contiguous(), tokens[:, 1:].reshape(-1).long()
     d = T_perp.shape[1]
     x = inner.embed_lookup(ids, p["T_S"], T_perp, pos, scale=d ** 0.5, flags=flags).reshape(-1, d)
-    _, y = inner.norm_block(x, w_pre=p["w_in"])
+    _, y = inner.norm_block(x, w_pre=p["w_in"], flags=flags)
     for i in range(layers):
         a, u = (y @ p[f"up{i}"]).split(ffn, dim=1)
         wide = (F.silu(a) * u) @ p[f"down{i}"]               # the block's output and its gate, side by side
-        x, y = inner.norm_block(x, wide[:, :d], wide[:, d:], p[f"post{i}"], p[f"pre{i}"], alpha)
+        x, y = inner.norm_block(x, wide[:, :d], wide[:, d:], p[f"post{i}"], p[f"pre{i}"], alpha, flags=flags)
     scores = (y @ (p["T_S"] + T_perp).t()).float()
     return F.cross_entropy(scores, target)
 

@@ -91,16 +91,16 @@ class _NormBlock(torch.autograd.Function):
     """x dense [n, d]; b and g rows of d, evenly spaced; weights dense [d]."""
 
     @staticmethod
-    def forward(ctx, x, b, g, w_post, w_pre, alpha, eps):
+    def forward(ctx, x, b, g, w_post, w_pre, alpha, eps, flags):
         n, d = x.shape
         act = (b if b is not None else x).dtype
         h = torch.empty_like(x) if b is not None else None
         y = torch.empty(n, d, dtype=act, device=x.device) if w_pre is not None else None
         stat = lambda w: None if w is None else torch.empty(n, dtype=torch.float32, device=x.device)  # noqa: E731
         r_post, r_pre = stat(w_post), stat(w_pre)
-        api.sl_norm_block(x, b, g, w_post, w_pre, n, d, alpha, eps, h, y, r_post, r_pre)
+        api.sl_norm_block(x, b, g, w_post, w_pre, n, d, alpha, eps, h, y, r_post, r_pre, flags)
         ctx.save_for_backward(h if h is not None else x, b, g, w_post, w_pre, r_post, r_pre)
-        ctx.args = (n, d, alpha)
+        ctx.args = (n, d, alpha, flags)
         ctx.set_materialize_grads(False)
         return h, y
 
@@ -108,9 +108,9 @@ class _NormBlock(torch.autograd.Function):
     @_once_differentiable
     def backward(ctx, dh, dy):
         h, b, g, w_post, w_pre, r_post, r_pre = ctx.saved_tensors
-        n, d, alpha = ctx.args
+        n, d, alpha, flags = ctx.args
         if dh is None and dy is None:
-            return (None,) * 7
+            return (None,) * 8
         dh, dy = _dense(dh), _dense(dy)
         if dy is None:                    # nothing came back through the second norm
             zero_pre, w_pre, r_pre = (None if w_pre is None else torch.zeros_like(w_pre)), None, None
@@ -119,10 +119,10 @@ class _NormBlock(torch.autograd.Function):
         db, dg = like(b), like(g)
         dw_post, dw_pre = like(w_post), like(w_pre)
         ws = torch.empty(api.sl_norm_block_grad_workspace(n, d), dtype=torch.uint8, device=h.device)
-        api.sl_norm_block_grad(dh, dy, h, b, g, w_post, w_pre, r_post, r_pre, n, d, alpha, dx, db, dg, dw_post, dw_pre, False, ws)
+        api.sl_norm_block_grad(dh, dy, h, b, g, w_post, w_pre, r_post, r_pre, n, d, alpha, dx, db, dg, dw_post, dw_pre, False, ws, flags)
         if dy is None:
             dw_pre = zero_pre
-        return dx, db, dg, dw_post, dw_pre, None, None
+        return dx, db, dg, dw_post, dw_pre, None, None, None
 
 
 def _rows(name: str, t, n: int, d: int):
@@ -135,17 +135,18 @@ def _rows(name: str, t, n: int, d: int):
     return v if v.stride(1) == 1 and (n <= 1 or v.stride(0) >= d) else v.contiguous()
 
 
-def norm_block(x, b=None, g=None, w_post=None, w_pre=None, alpha: float = 1.0, eps: float = 1e-6):
+def norm_block(x, b=None, g=None, w_post=None, w_pre=None, alpha: float = 1.0, eps: float = 1e-6, flags=None):
     """(h, y): h = x + alpha sigmoid(g) norm(b) w_post and y = norm(h) w_pre, each term left out where its tensor is
     None (no b: h is None and y = norm(x) w_pre; no w_pre: y is None).  x, b and g: rows of one width in any shape, as many of
-    each; h and y have x's.  Differentiable in every tensor; a second derivative raises RuntimeError."""
+    each; h and y have x's.  flags: int32 device word; SL_FLAG_TIMEOUT in it, from the forward or the backward pass, says that
+    their results are not to be used.  Differentiable in every tensor; a second derivative raises RuntimeError."""
     d = x.shape[-1] if x.dim() else 0
     if d < 1:
         raise ValueError(f"x: expected rows, got {list(x.shape)}")
     n = x.numel() // d
     weight = lambda name, w: None if w is None else _rows(name, w, 1, d).reshape(d)  # noqa: E731
     h, y = _NormBlock.apply(_dense(x.reshape(n, d)), _rows("b", b, n, d), _rows("g", g, n, d), weight("w_post", w_post),
-                            weight("w_pre", w_pre), float(alpha), float(eps))
+                            weight("w_pre", w_pre), float(alpha), float(eps), flags)
     return (None if h is None else h.view(x.shape)), (None if y is None else y.view(x.shape))
 
 

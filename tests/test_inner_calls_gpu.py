@@ -117,3 +117,23 @@ def test_a_second_derivative_of_the_lookup():
     first, = torch.autograd.grad(inner.embed_lookup(ids, T).sum(), T, create_graph=True)
     got, = torch.autograd.grad((first ** 2).sum() + (T ** 2).sum(), T)        # and does not depend on the table
     assert torch.equal(got, 2 * T)
+
+
+def test_flags_of_the_norm_block_arrive_from_both_passes():
+    # a row of several CTAs whose waits give up at once: nothing is left in flight, and the outputs are not to be used
+    n, d = 64, 8192
+    x, b, w = (_randn(*s, seed=i, dtype=torch.bfloat16).requires_grad_() for i, s in enumerate([(n, d), (n, d), (d,)]))
+    forward, backward = (torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(2))
+    try:
+        api.sl_debug_set_wait_limit(-1)
+        inner.norm_block(x, b, None, w, w, flags=forward)
+        torch.cuda.synchronize()
+        api.sl_debug_set_wait_limit(0)
+        h, y = inner.norm_block(x, b, None, w, w, flags=backward)
+        assert int(forward.item()) == api.SL_FLAG_TIMEOUT and int(backward.item()) == 0
+        api.sl_debug_set_wait_limit(-1)
+        (h.sum() + y.sum()).backward()
+        torch.cuda.synchronize()
+        assert int(backward.item()) == api.SL_FLAG_TIMEOUT
+    finally:
+        api.sl_debug_set_wait_limit(0)
