@@ -188,9 +188,9 @@ def _ptr_table(ts: Sequence) -> ctypes.Array:
     return a
 
 
-def _stream(stream) -> int:
+def _stream(stream, device: Optional[int] = None) -> int:
     if stream is None:                     # the handle alone: building a Stream object costs 3 us a call
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device)
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -338,7 +338,8 @@ def sl_unpack_idx12(packed, layout, chunk: int, k: int, idx, stream=None) -> Non
 
 # ---------------------------------------------------------------------------
 # the inner step (Eq. 1).  Element types come from the tensors; a tensor of another type, on the host, or too
-# small for what the call touches raises ValueError before anything is launched (csrc/sl_args.cpp).
+# small for what the call touches, or on another device than the current one (where the launch goes) raises ValueError before
+# anything is launched (csrc/sl_args.cpp).
 # ---------------------------------------------------------------------------
 _F32, _BF16, _FLOAT, _I32, _I8, _U8 = 1, 2, 3, 4, 8, 16          # bits of a type mask
 _TYPES = {_F32: SL_F32, _BF16: SL_BF16}
@@ -370,12 +371,13 @@ def sl_adamw(theta, grad, m, v, layout, lr: float, beta1: float, beta2: float, e
              grad_scale=None, copy=None, flags=None, stream=None) -> None:
     """theta, grad: float32 or bfloat16; m, v: float32; copy: bfloat16 copy of a float32 theta, written."""
     c = _args or _checks()
+    dev = c.device()
     lay = _layout(layout)
     n = lay.n_total
     keep, dec = _decay(decay, len(lay.offsets) - 1)
-    _check(load().sl_adamw(c.ptr(theta, "theta", n, _FLOAT), _TYPES.get(c.type(theta), -1), c.ptr(grad, "grad", n, _FLOAT), _TYPES.get(c.type(grad), -1),
-                           c.ptr(m, "m", n, _F32), c.ptr(v, "v", n, _F32), c.ptr(copy, "copy", n, _BF16), lay.ref(), dec, lr, beta1,
-                           beta2, eps, step, c.ptr(grad_scale, "grad_scale", 1, _F32), c.ptr(flags, "flags", 1, _I32), _stream(stream)),
+    _check(load().sl_adamw(c.ptr(theta, "theta", n, _FLOAT, dev), _TYPES.get(c.type(theta), -1), c.ptr(grad, "grad", n, _FLOAT, dev), _TYPES.get(c.type(grad), -1),
+                           c.ptr(m, "m", n, _F32, dev), c.ptr(v, "v", n, _F32, dev), c.ptr(copy, "copy", n, _BF16, dev), lay.ref(), dec, lr, beta1,
+                           beta2, eps, step, c.ptr(grad_scale, "grad_scale", 1, _F32, dev), c.ptr(flags, "flags", 1, _I32, dev), _stream(stream, dev)),
            "sl_adamw")
 
 
@@ -383,34 +385,37 @@ def sl_adamw8_blocks(layout) -> int:
     return int(load().sl_adamw8_blocks(_layout(layout).ref()))
 
 
-def _states8(m8, v8, m_scale, v_scale, lay):
+def _states8(m8, v8, m_scale, v_scale, lay, dev):
     c, n, nb = _args or _checks(), lay.n_total, lay.state_blocks()
-    return (c.ptr(m8, "m8", n, _I8), c.ptr(v8, "v8", n, _U8), c.ptr(m_scale, "m_scale", nb, _F32), c.ptr(v_scale, "v_scale", nb, _F32))
+    return (c.ptr(m8, "m8", n, _I8, dev), c.ptr(v8, "v8", n, _U8, dev), c.ptr(m_scale, "m_scale", nb, _F32, dev), c.ptr(v_scale, "v_scale", nb, _F32, dev))
 
 
 def sl_adamw8(theta, grad, m8, v8, m_scale, v_scale, layout, lr: float, beta1: float, beta2: float, eps: float, step: int,
               decay=None, grad_scale=None, copy=None, flags=None, stream=None) -> None:
     """As sl_adamw with the moments in 8 bits (m8: int8, v8: uint8, one float32 scale per block of 256 each)."""
     c = _args or _checks()
+    dev = c.device()
     lay = _layout(layout)
     n = lay.n_total
     keep, dec = _decay(decay, len(lay.offsets) - 1)
-    _check(load().sl_adamw8(c.ptr(theta, "theta", n, _FLOAT), _TYPES.get(c.type(theta), -1), c.ptr(grad, "grad", n, _FLOAT), _TYPES.get(c.type(grad), -1),
-                            *_states8(m8, v8, m_scale, v_scale, lay), c.ptr(copy, "copy", n, _BF16), lay.ref(), dec, lr, beta1, beta2,
-                            eps, step, c.ptr(grad_scale, "grad_scale", 1, _F32), c.ptr(flags, "flags", 1, _I32), _stream(stream)),
+    _check(load().sl_adamw8(c.ptr(theta, "theta", n, _FLOAT, dev), _TYPES.get(c.type(theta), -1), c.ptr(grad, "grad", n, _FLOAT, dev), _TYPES.get(c.type(grad), -1),
+                            *_states8(m8, v8, m_scale, v_scale, lay, dev), c.ptr(copy, "copy", n, _BF16, dev), lay.ref(), dec, lr, beta1, beta2,
+                            eps, step, c.ptr(grad_scale, "grad_scale", 1, _F32, dev), c.ptr(flags, "flags", 1, _I32, dev), _stream(stream, dev)),
            "sl_adamw8")
 
 
 def sl_adamw8_pack(m, v, layout, m8, v8, m_scale, v_scale, stream=None) -> None:
     c, lay = _args or _checks(), _layout(layout)
-    _check(load().sl_adamw8_pack(c.ptr(m, "m", lay.n_total, _F32), c.ptr(v, "v", lay.n_total, _F32), lay.ref(),
-                                 *_states8(m8, v8, m_scale, v_scale, lay), _stream(stream)), "sl_adamw8_pack")
+    dev = c.device()
+    _check(load().sl_adamw8_pack(c.ptr(m, "m", lay.n_total, _F32, dev), c.ptr(v, "v", lay.n_total, _F32, dev), lay.ref(),
+                                 *_states8(m8, v8, m_scale, v_scale, lay, dev), _stream(stream, dev)), "sl_adamw8_pack")
 
 
 def sl_adamw8_unpack(m8, v8, m_scale, v_scale, layout, m, v, stream=None) -> None:
     c, lay = _args or _checks(), _layout(layout)
-    _check(load().sl_adamw8_unpack(*_states8(m8, v8, m_scale, v_scale, lay), lay.ref(), c.ptr(m, "m", lay.n_total, _F32),
-                                   c.ptr(v, "v", lay.n_total, _F32), _stream(stream)), "sl_adamw8_unpack")
+    dev = c.device()
+    _check(load().sl_adamw8_unpack(*_states8(m8, v8, m_scale, v_scale, lay, dev), lay.ref(), c.ptr(m, "m", lay.n_total, _F32, dev),
+                                   c.ptr(v, "v", lay.n_total, _F32, dev), _stream(stream, dev)), "sl_adamw8_unpack")
 
 
 def alloc_states8(layout, device="cuda"):
@@ -423,11 +428,12 @@ def alloc_states8(layout, device="cuda"):
 
 def sl_embed_lookup(ids, T_S, T_perp, pos, scale: float, n_tok: int, L: int, V: int, d: int, X, flags=None, stream=None) -> None:
     c = _args or _checks()
-    table = c.ptr(T_S, "T_S", V * d, _FLOAT)
+    dev = c.device()
+    table = c.ptr(T_S, "T_S", V * d, _FLOAT, dev)
     tt = c.type(T_S)
-    _check(load().sl_embed_lookup(c.ptr(ids, "ids", n_tok, _I32), table, c.ptr(T_perp, "T_perp", V * d, tt), c.ptr(pos, "pos", L * d, tt),
-                                  _TYPES.get(tt, -1), scale, n_tok, L, V, d, c.ptr(X, "X", n_tok * d, _FLOAT), _TYPES.get(c.type(X), -1),
-                                  c.ptr(flags, "flags", 1, _I32), _stream(stream)), "sl_embed_lookup")
+    _check(load().sl_embed_lookup(c.ptr(ids, "ids", n_tok, _I32, dev), table, c.ptr(T_perp, "T_perp", V * d, tt, dev), c.ptr(pos, "pos", L * d, tt, dev),
+                                  _TYPES.get(tt, -1), scale, n_tok, L, V, d, c.ptr(X, "X", n_tok * d, _FLOAT, dev), _TYPES.get(c.type(X), -1),
+                                  c.ptr(flags, "flags", 1, _I32, dev), _stream(stream, dev)), "sl_embed_lookup")
 
 
 def sl_embed_grad_workspace(n_tok: int, V: int, d: int) -> int:
@@ -437,12 +443,13 @@ def sl_embed_grad_workspace(n_tok: int, V: int, d: int) -> int:
 def sl_embed_grad(ids, dX, scale: float, n_tok: int, L: int, V: int, d: int, dT, dpos, acc: bool, ws, flags=None, stream=None) -> None:
     """ws: uint8 workspace of sl_embed_grad_workspace(n_tok, V, d) bytes."""
     c, lib = _args or _checks(), load()
-    table = c.ptr(dT, "dT", V * d, _FLOAT)
+    dev = c.device()
+    table = c.ptr(dT, "dT", V * d, _FLOAT, dev)
     tt = c.type(dT)
-    _check(lib.sl_embed_grad(c.ptr(ids, "ids", n_tok, _I32), c.ptr(dX, "dX", n_tok * d, _FLOAT), _TYPES.get(c.type(dX), -1), scale, n_tok, L, V, d,
-                             table, c.ptr(dpos, "dpos", L * d, tt), _TYPES.get(tt, -1), 1 if acc else 0,
-                             c.ptr(ws, "ws", lib.sl_embed_grad_workspace(n_tok, V, d), _U8), c.ptr(flags, "flags", 1, _I32),
-                             _stream(stream)), "sl_embed_grad")
+    _check(lib.sl_embed_grad(c.ptr(ids, "ids", n_tok, _I32, dev), c.ptr(dX, "dX", n_tok * d, _FLOAT, dev), _TYPES.get(c.type(dX), -1), scale, n_tok, L, V, d,
+                             table, c.ptr(dpos, "dpos", L * d, tt, dev), _TYPES.get(tt, -1), 1 if acc else 0,
+                             c.ptr(ws, "ws", lib.sl_embed_grad_workspace(n_tok, V, d), _U8, dev), c.ptr(flags, "flags", 1, _I32, dev),
+                             _stream(stream, dev)), "sl_embed_grad")
 
 
 def _norm_types(c, x, b, y, w_post, w_pre):
@@ -455,13 +462,14 @@ def sl_norm_block(x, b, g, w_post, w_pre, n: int, d: int, alpha: float, eps: flo
                   flags=None, stream=None) -> None:
     """b and g may be columns of wider matrices (dense rows, evenly spaced); the rest is dense."""
     c = _args or _checks()
+    dev = c.device()
     rt, at, wt = _norm_types(c, x, b, y, w_post, w_pre)
-    (pb, ldb), (pg, ldg) = c.rows(b, "b", n, d, at), c.rows(g, "g", n, d, at)
+    (pb, ldb), (pg, ldg) = c.rows(b, "b", n, d, at, dev), c.rows(g, "g", n, d, at, dev)
     nd = n * d
-    _check(load().sl_norm_block(c.ptr(x, "x", nd, _FLOAT), pb, pg, _TYPES.get(rt, -1), _TYPES.get(at, -1), c.ptr(w_post, "w_post", d, wt),
-                                c.ptr(w_pre, "w_pre", d, wt), _TYPES.get(wt, -1), n, d, ldb, ldg, alpha, eps, c.ptr(h, "h", nd, rt),
-                                c.ptr(y, "y", nd, at), c.ptr(r_post, "r_post", n, _F32), c.ptr(r_pre, "r_pre", n, _F32),
-                                c.ptr(flags, "flags", 1, _I32), _stream(stream)), "sl_norm_block")
+    _check(load().sl_norm_block(c.ptr(x, "x", nd, _FLOAT, dev), pb, pg, _TYPES.get(rt, -1), _TYPES.get(at, -1), c.ptr(w_post, "w_post", d, wt, dev),
+                                c.ptr(w_pre, "w_pre", d, wt, dev), _TYPES.get(wt, -1), n, d, ldb, ldg, alpha, eps, c.ptr(h, "h", nd, rt, dev),
+                                c.ptr(y, "y", nd, at, dev), c.ptr(r_post, "r_post", n, _F32, dev), c.ptr(r_pre, "r_pre", n, _F32, dev),
+                                c.ptr(flags, "flags", 1, _I32, dev), _stream(stream, dev)), "sl_norm_block")
 
 
 def sl_norm_block_grad_workspace(n: int, d: int) -> int:
@@ -472,17 +480,18 @@ def sl_norm_block_grad(dh, dy, h, b, g, w_post, w_pre, r_post, r_pre, n: int, d:
                        acc: bool, ws, flags=None, stream=None) -> None:
     """db and dg have the row distances of b and g; ws: uint8 workspace of sl_norm_block_grad_workspace(n, d) bytes."""
     c, lib = _args or _checks(), load()
+    dev = c.device()
     rt, at, wt = _norm_types(c, h, b, dy, w_post, w_pre)
-    (pb, ldb), (pg, ldg) = c.rows(b, "b", n, d, at), c.rows(g, "g", n, d, at)
-    (pdb, ldb2), (pdg, ldg2) = c.rows(db, "db", n, d, at), c.rows(dg, "dg", n, d, at)
+    (pb, ldb), (pg, ldg) = c.rows(b, "b", n, d, at, dev), c.rows(g, "g", n, d, at, dev)
+    (pdb, ldb2), (pdg, ldg2) = c.rows(db, "db", n, d, at, dev), c.rows(dg, "dg", n, d, at, dev)
     if (db is not None and ldb != ldb2) or (dg is not None and ldg != ldg2):
         raise ValueError("db and dg: expected the row distances of b and g")
     nd, need = n * d, lib.sl_norm_block_grad_workspace(n, d)
-    _check(lib.sl_norm_block_grad(c.ptr(dh, "dh", nd, rt), c.ptr(dy, "dy", nd, at), c.ptr(h, "h", nd, _FLOAT), pb, pg, _TYPES.get(rt, -1),
-                                  _TYPES.get(at, -1), c.ptr(w_post, "w_post", d, wt), c.ptr(w_pre, "w_pre", d, wt), _TYPES.get(wt, -1),
-                                  c.ptr(r_post, "r_post", n, _F32), c.ptr(r_pre, "r_pre", n, _F32), n, d, ldb, ldg, alpha,
-                                  c.ptr(dx, "dx", nd, rt), pdb, pdg, c.ptr(dw_post, "dw_post", d, wt), c.ptr(dw_pre, "dw_pre", d, wt),
-                                  1 if acc else 0, c.ptr(ws, "ws", need, _U8), c.ptr(flags, "flags", 1, _I32), _stream(stream)),
+    _check(lib.sl_norm_block_grad(c.ptr(dh, "dh", nd, rt, dev), c.ptr(dy, "dy", nd, at, dev), c.ptr(h, "h", nd, _FLOAT, dev), pb, pg, _TYPES.get(rt, -1),
+                                  _TYPES.get(at, -1), c.ptr(w_post, "w_post", d, wt, dev), c.ptr(w_pre, "w_pre", d, wt, dev), _TYPES.get(wt, -1),
+                                  c.ptr(r_post, "r_post", n, _F32, dev), c.ptr(r_pre, "r_pre", n, _F32, dev), n, d, ldb, ldg, alpha,
+                                  c.ptr(dx, "dx", nd, rt, dev), pdb, pdg, c.ptr(dw_post, "dw_post", d, wt, dev), c.ptr(dw_pre, "dw_pre", d, wt, dev),
+                                  1 if acc else 0, c.ptr(ws, "ws", need, _U8, dev), c.ptr(flags, "flags", 1, _I32, dev), _stream(stream, dev)),
            "sl_norm_block_grad")
 
 

@@ -137,3 +137,44 @@ def test_flags_of_the_norm_block_arrive_from_both_passes():
         assert int(backward.item()) == api.SL_FLAG_TIMEOUT
     finally:
         api.sl_debug_set_wait_limit(0)
+
+
+class _OtherDevice:
+    """The argument checks as they are when another device than that of the tensors is current."""
+
+    def __init__(self, checks):
+        self.checks = checks
+
+    def __getattr__(self, name):
+        return getattr(self.checks, name)
+
+    def device(self):
+        return torch.cuda.current_device() + 1
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    n, d = 4, 8
+    x, w, r = _randn(n, d), _randn(d), _randn(n)
+    ids, ws = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
+    s8, lay = api.alloc_states8([0, 32]), api.Layout([0, 32])
+    new = lambda: torch.empty(n, d, device="cuda")  # noqa: E731
+    calls = [lambda: api.sl_adamw(new(), new(), new(), new(), lay, 1e-3, 0.9, 0.95, 1e-8, 1),
+             lambda: api.sl_adamw8(new(), new(), *s8, lay, 1e-3, 0.9, 0.95, 1e-8, 1),
+             lambda: api.sl_adamw8_pack(x, x.abs(), lay, *s8),
+             lambda: api.sl_adamw8_unpack(*s8, lay, new(), new()),
+             lambda: api.sl_embed_lookup(ids, x, None, None, 1.0, n, n, n, d, new()),
+             lambda: api.sl_embed_grad(ids, x, 1.0, n, n, n, d, new(), None, False, ws),
+             lambda: api.sl_norm_block(x, x, None, None, w, n, d, 1.0, 1e-6, new(), new()),
+             lambda: api.sl_norm_block_grad(x, None, x, x, None, None, None, None, None, n, d, 1.0, new(), new(), None, None, None, False, ws)]
+    for call in calls:
+        call()
+    checks = api._checks()
+    assert checks.device() == torch.cuda.current_device()
+    with pytest.raises(ValueError):
+        checks.ptr(x, "x", 1, 1, checks.device() + 1)
+    with pytest.raises(ValueError):
+        checks.rows(x, "x", n, d, 1, checks.device() + 1)
+    monkeypatch.setattr(api, "_args", _OtherDevice(checks))
+    for call in calls:
+        with pytest.raises(ValueError, match="current CUDA device"):
+            call()
