@@ -1,6 +1,6 @@
 """The inner step of a replica (Eq. 1) on torch tensors: autograd functions over the embedding lookup and the norm
 block, and the AdamW step over an arena.  Marshalling only: every operation is one of the library's calls on the
-current stream; outputs and workspaces come from torch's allocator.
+current stream of its tensors' device; outputs and workspaces come from torch's allocator.
 
     x = embed_lookup(ids, T_S, T_perp, pos)                 # X^(0) of sections 2.3 / 2.4
     _, y = norm_block(x, None, None, None, w_in)            # norm before the first block
@@ -57,7 +57,8 @@ class _EmbedLookup(torch.autograd.Function):
         V, d = T_S.shape
         n = ids.numel()
         X = torch.empty(n, d, dtype=out_dtype or T_S.dtype, device=T_S.device)
-        api.sl_embed_lookup(ids, T_S, T_perp, pos, scale, n, L, V, d, X, flags)
+        with torch.cuda.device_of(T_S):
+            api.sl_embed_lookup(ids, T_S, T_perp, pos, scale, n, L, V, d, X, flags)
         ctx.save_for_backward(ids)
         ctx.sizes = (n, L, V, d, scale, T_S.dtype, flags)
         return X
@@ -71,7 +72,8 @@ class _EmbedLookup(torch.autograd.Function):
         dT = torch.empty(V, d, dtype=dtype, device=dX.device)
         dpos = torch.empty(L, d, dtype=dtype, device=dX.device) if need_pos else None
         ws = torch.empty(api.sl_embed_grad_workspace(n, V, d), dtype=torch.uint8, device=dX.device)
-        api.sl_embed_grad(ids, _dense(dX), scale, n, L, V, d, dT, dpos, False, ws, flags)
+        with torch.cuda.device_of(ids):
+            api.sl_embed_grad(ids, _dense(dX), scale, n, L, V, d, dT, dpos, False, ws, flags)
         return None, (dT if need_s else None), (dT if need_p else None), dpos, None, None, None, None
 
 
@@ -98,7 +100,8 @@ class _NormBlock(torch.autograd.Function):
         y = torch.empty(n, d, dtype=act, device=x.device) if w_pre is not None else None
         stat = lambda w: None if w is None else torch.empty(n, dtype=torch.float32, device=x.device)  # noqa: E731
         r_post, r_pre = stat(w_post), stat(w_pre)
-        api.sl_norm_block(x, b, g, w_post, w_pre, n, d, alpha, eps, h, y, r_post, r_pre, flags)
+        with torch.cuda.device_of(x):
+            api.sl_norm_block(x, b, g, w_post, w_pre, n, d, alpha, eps, h, y, r_post, r_pre, flags)
         ctx.save_for_backward(h if h is not None else x, b, g, w_post, w_pre, r_post, r_pre)
         ctx.args = (n, d, alpha, flags)
         ctx.set_materialize_grads(False)
@@ -119,7 +122,8 @@ class _NormBlock(torch.autograd.Function):
         db, dg = like(b), like(g)
         dw_post, dw_pre = like(w_post), like(w_pre)
         ws = torch.empty(api.sl_norm_block_grad_workspace(n, d), dtype=torch.uint8, device=h.device)
-        api.sl_norm_block_grad(dh, dy, h, b, g, w_post, w_pre, r_post, r_pre, n, d, alpha, dx, db, dg, dw_post, dw_pre, False, ws, flags)
+        with torch.cuda.device_of(h):
+            api.sl_norm_block_grad(dh, dy, h, b, g, w_post, w_pre, r_post, r_pre, n, d, alpha, dx, db, dg, dw_post, dw_pre, False, ws, flags)
         if dy is None:
             dw_pre = zero_pre
         return dx, db, dg, dw_post, dw_pre, None, None, None
@@ -172,15 +176,17 @@ class AdamW:
         in `flags`; the step count goes on."""
         self.steps += 1
         call = api.sl_adamw8 if self.bits == 8 else api.sl_adamw
-        call(self.theta, grad, *self.states, self.layout, self.lr, *self.betas, self.eps, self.steps, decay=self.decay,
-             grad_scale=grad_scale, copy=self.copy, flags=self.flags, stream=stream)
+        with torch.cuda.device_of(self.theta):
+            call(self.theta, grad, *self.states, self.layout, self.lr, *self.betas, self.eps, self.steps, decay=self.decay,
+                 grad_scale=grad_scale, copy=self.copy, flags=self.flags, stream=stream)
 
     def moments(self):
         """(m, v) as float32: the moments themselves, or the values that their codes stand for."""
         if self.bits == 32:
             return self.states
         m, v = (torch.empty(self.layout.n_total, dtype=torch.float32, device=self.theta.device) for _ in range(2))
-        api.sl_adamw8_unpack(*self.states, self.layout, m, v)
+        with torch.cuda.device_of(self.theta):
+            api.sl_adamw8_unpack(*self.states, self.layout, m, v)
         return m, v
 
     def load_moments(self, m: torch.Tensor, v: torch.Tensor, steps: int) -> None:
@@ -189,5 +195,6 @@ class AdamW:
             self.states[0].copy_(m)
             self.states[1].copy_(v)
         else:
-            api.sl_adamw8_pack(m, v, self.layout, *self.states)
+            with torch.cuda.device_of(self.theta):
+                api.sl_adamw8_pack(m, v, self.layout, *self.states)
         self.steps = steps
