@@ -852,8 +852,11 @@ cudaError_t embed_grad_typed(const EmbedGradArgs& a, cudaStream_t st, int sms) {
   s.passes = (bits + kDigitBits - 1) / kDigitBits;
   s.bits = (bits + s.passes - 1) / s.passes;
   for (int i = 0; i < 2; ++i) s.list[i] = reinterpret_cast<uint2*>(ws + w.list[i]);
-  const size_t smem = ((size_t)((kSortWarps + 1) << s.bits) + kSortWarps) * 4;
-  if ((e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
+  auto sort_smem = [](int digit_bits) { return ((size_t)((kSortWarps + 1) << digit_bits) + kSortWarps) * 4; };
+  const size_t smem = sort_smem(s.bits);
+  // the limit belongs to the process: the same value in every call, so that none lowers it under another thread's launch
+  if ((e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sort_smem(kDigitBits))) != cudaSuccess)
+    return e;
   if ((e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
