@@ -225,7 +225,10 @@ int sl_embed_lookup(const int32_t* ids, const void* T_S, const void* T_perp, con
   return status(launch_embed_lookup(a, table_type, x_type, (cudaStream_t)stream));
 }
 
-uint64_t sl_embed_grad_workspace(uint64_t n_tok, uint64_t V, uint32_t d) { return embed_grad_workspace(n_tok, V, d); }
+uint64_t sl_embed_grad_workspace(uint64_t n_tok, uint64_t V, uint32_t d) {
+  if (d < 1 || d > 0x7FFFFFFFu || n_tok > 0x7FFFFFFFull) return 0;         // sizes that the call refuses
+  return embed_grad_workspace(n_tok, V, d);
+}
 
 int sl_embed_grad(const int32_t* ids, const void* dX, int dx_type, float scale, uint64_t n_tok, uint32_t L, uint64_t V, uint32_t d,
                   void* dT, void* dpos, int dt_type, int acc, void* ws, uint32_t* flags, void* stream) {
