@@ -325,7 +325,7 @@ int sl_embed_lookup(const int32_t* ids, const void* T_S, const void* T_perp, con
  * are of dt_type.  Ids outside [0, V) contribute nothing and raise SL_FLAG_BAD_INDEX.  Rows without a
  * token: zeros with acc = 0, untouched with acc = 1.
  * ws: DEVICE workspace of sl_embed_grad_workspace(n_tok, V, d) bytes (0 for sizes that are refused), 32-byte aligned; its
- * contents before and after the call do not matter.  n_tok, V < 2^31. */
+ * contents before and after the call do not matter.  n_tok, V < 2^31; widths above 65535 * 64 may be SL_ERR_UNSUPPORTED. */
 uint64_t sl_embed_grad_workspace(uint64_t n_tok, uint64_t V, uint32_t d);
 int sl_embed_grad(const int32_t* ids, const void* dX, int dx_type, float scale, uint64_t n_tok, uint32_t L, uint64_t V,
                   uint32_t d, void* dT, void* dpos, int dt_type, int acc, void* ws, uint32_t* flags, void* stream);

@@ -191,6 +191,7 @@ struct EmbedGradArgs {
 cudaError_t launch_embed_lookup(const LookupArgs& a, int table_type, int x_type, cudaStream_t st);
 cudaError_t launch_embed_grad(const EmbedGradArgs& a, int dx_type, int dt_type, cudaStream_t st);
 uint64_t embed_grad_workspace(uint64_t n_tok, uint64_t V, uint32_t d);
+bool embed_grad_fits(const EmbedGradArgs& a, int dx_type, int dt_type);      // a grid holds its columns
 
 // ---------------------------------------------------------------------------
 // norm block

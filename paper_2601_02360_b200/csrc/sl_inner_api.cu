@@ -241,6 +241,7 @@ int sl_embed_grad(const int32_t* ids, const void* dX, int dx_type, float scale, 
   if (n_tok > 0x7FFFFFFFull || V > 0x7FFFFFFFull || d > 0x7FFFFFFFu) return SL_ERR_UNSUPPORTED;
   if (n_tok == 0 && acc) return SL_OK;
   EmbedGradArgs a{ids, dX, dT, dpos, ws, flags, scale, (uint32_t)n_tok, L < 1 ? 1u : L, (uint32_t)V, d, acc ? 1 : 0};
+  if (!embed_grad_fits(a, dx_type, dt_type)) return SL_ERR_UNSUPPORTED;
   return status(launch_embed_grad(a, dx_type, dt_type, (cudaStream_t)stream));
 }
 

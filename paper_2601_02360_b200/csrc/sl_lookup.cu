@@ -935,11 +935,23 @@ cudaError_t launch_embed_lookup(const LookupArgs& a, int table_type, int x_type,
 
 uint64_t embed_grad_workspace(uint64_t n_tok, uint64_t, uint32_t d) { return Workspace(n_tok, d).bytes; }
 
+static bool embed_grad_vectors(const EmbedGradArgs& a, int dx_type, int dt_type) {
+  return a.d % 8 == 0 && vector_aligned(a.dX, dx_type) && vector_aligned(a.dT, dt_type) && vector_aligned(a.dpos, dt_type);
+}
+
+// the join kernel of many tokens deals out columns along a grid's second axis, which ends at 65,535 (few tokens' positions are cut
+// only where rows are narrow)
+bool embed_grad_fits(const EmbedGradArgs& a, int dx_type, int dt_type) {
+  if (a.n_tok <= kDirectMost) return true;
+  const uint32_t columns = embed_grad_vectors(a, dx_type, dt_type) ? kSide<8> * 8 : kSide<1>;
+  return (a.d + columns - 1) / columns <= 65535;
+}
+
 cudaError_t launch_embed_grad(const EmbedGradArgs& a, int dx_type, int dt_type, cudaStream_t st) {
   cudaError_t err;
   const int sms = sm_count(&err);
   if (err != cudaSuccess) return err;
-  const bool vec = a.d % 8 == 0 && vector_aligned(a.dX, dx_type) && vector_aligned(a.dT, dt_type) && vector_aligned(a.dpos, dt_type);
+  const bool vec = embed_grad_vectors(a, dx_type, dt_type);
   return with_type(dx_type, [&](auto dx) {
     return with_type(dt_type, [&](auto dt) {
       using DX = decltype(dx);

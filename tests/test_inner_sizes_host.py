@@ -23,3 +23,11 @@ def test_the_workspace_of_a_size_that_is_refused(lib, n, d):
     code = f"import sys; sys.path.insert(0, {ROOT!r}); from paper_2601_02360_b200 import api; print(api.load().sl_embed_grad_workspace({n}, 10, {d}))"
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True)
     assert r.returncode == 0 and int(r.stdout) == 0, (r.returncode, r.stderr[-300:])
+
+
+def test_widths_that_no_grid_holds_are_refused(lib):
+    def call(d, dX=P):
+        return lib.sl_embed_grad(P, dX, 0, 1.0, 5000, 1, 10, d, P, 0, 0, 1, P, 0, 0)
+    UNS = api.SL_ERR_UNSUPPORTED
+    assert call(65535 * 64 + 1) == UNS and call(65535 * 64 + 8, dX=P + 4) == UNS      # single elements: 64 columns to a CTA
+    assert call(65535 * 128 + 8) == UNS and call(1 << 31) == UNS                      # vectors: 128
