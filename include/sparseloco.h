@@ -255,6 +255,8 @@ int sl_round_tf32(float* x, uint64_t n, void* stream);
  * freely: SL_F32 is float, SL_BF16 the upper half of one (uint16_t).  Arithmetic is float32 whatever the
  * storage; storing to bfloat16 rounds once, to nearest even.  float arrays that start on 32 bytes and
  * bfloat16 ones that start on 16 are moved in vectors; any other start gives the same results more slowly.
+ * No tokens, rows or elements at all: arrays that would be empty may be NULL, and nothing is written but the zeros of sums over
+ * nothing.
  * ------------------------------------------------------------------------------------------------ */
 enum { SL_F32 = 0, SL_BF16 = 1 };
 

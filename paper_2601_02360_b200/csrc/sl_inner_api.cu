@@ -86,7 +86,8 @@ int with_args(const AdamwArgs<1>& common, const sl_layout* L, uint32_t block, ui
 int adamw_common(AdamwArgs<1>& a, void* theta, int theta_type, const void* grad, int grad_type, uint16_t* copy, const sl_layout* L,
                  uint32_t block, uint32_t vec, const float* decay, double lr, double beta1, double beta2, double eps, uint64_t step,
                  const float* grad_scale, uint32_t* flags) {
-  if (!theta || !grad || !type_ok(theta_type) || !type_ok(grad_type) || (copy && theta_type != SL_F32)) return SL_ERR_INVALID_ARG;
+  if (!type_ok(theta_type) || !type_ok(grad_type) || (copy && theta_type != SL_F32)) return SL_ERR_INVALID_ARG;
+  if (!L || (L->n_total > 0 && (!theta || !grad))) return SL_ERR_INVALID_ARG;
   if (!std::isfinite(lr) || lr < 0 || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps > 0) || !(eps <= FLT_MAX) ||
       (float)eps == 0.0f || step < 1)
     return SL_ERR_INVALID_ARG;
@@ -118,8 +119,8 @@ int adamw_common(AdamwArgs<1>& a, void* theta, int theta_type, const void* grad,
   return SL_OK;
 }
 
-int states8_check(const int8_t* m8, const uint8_t* v8, const float* m_scale, const float* v_scale) {
-  if (!m8 || !v8 || !m_scale || !v_scale) return SL_ERR_INVALID_ARG;
+int states8_check(const sl_layout* L, const int8_t* m8, const uint8_t* v8, const float* m_scale, const float* v_scale) {
+  if (!L || (L->n_total > 0 && (!m8 || !v8 || !m_scale || !v_scale))) return SL_ERR_INVALID_ARG;
   return is_aligned(m_scale, 4) && is_aligned(v_scale, 4) ? SL_OK : SL_ERR_ALIGNMENT;
 }
 
@@ -137,9 +138,9 @@ AdamwArgs<1> convert_args(float* m, float* v, int8_t* m8, uint8_t* v8, float* m_
 
 int convert_check(const float* m, const float* v, const sl_layout* L, const int8_t* m8, const uint8_t* v8, const float* m_scale,
                   const float* v_scale) {
-  if (!m || !v) return SL_ERR_INVALID_ARG;
-  int rc = states8_check(m8, v8, m_scale, v_scale);
+  int rc = states8_check(L, m8, v8, m_scale, v_scale);
   if (rc != SL_OK) return rc;
+  if (L->n_total > 0 && (!m || !v)) return SL_ERR_INVALID_ARG;
   if ((rc = check_layout(L, SL_STATE_BLOCK, 1)) != SL_OK) return rc;
   return is_aligned(m, 4) && is_aligned(v, 4) ? SL_OK : SL_ERR_ALIGNMENT;
 }
@@ -157,7 +158,7 @@ int sl_adamw(void* theta, int theta_type, const void* grad, int grad_type, float
              const float* decay, double lr, double beta1, double beta2, double eps, uint64_t step, const float* grad_scale,
              uint32_t* flags, void* stream) {
   AdamwArgs<1> a;
-  if (!m || !v || !L) return SL_ERR_INVALID_ARG;
+  if (!L || (L->n_total > 0 && (!m || !v))) return SL_ERR_INVALID_ARG;
   const uint32_t block = adamw_block(L->n_total);
   const int rc = adamw_common(a, theta, theta_type, grad, grad_type, copy, L, block, 4, decay, lr, beta1, beta2, eps, step,
                               grad_scale, flags);
@@ -181,7 +182,7 @@ int sl_adamw8(void* theta, int theta_type, const void* grad, int grad_type, int8
               uint16_t* copy, const sl_layout* L, const float* decay, double lr, double beta1, double beta2, double eps,
               uint64_t step, const float* grad_scale, uint32_t* flags, void* stream) {
   AdamwArgs<1> a;
-  int rc = states8_check(m8, v8, m_scale, v_scale);
+  int rc = states8_check(L, m8, v8, m_scale, v_scale);
   if (rc != SL_OK) return rc;
   rc = adamw_common(a, theta, theta_type, grad, grad_type, copy, L, SL_STATE_BLOCK, 8, decay, lr, beta1, beta2, eps, step, grad_scale,
                     flags);
@@ -214,7 +215,7 @@ int sl_adamw8_unpack(const int8_t* m8, const uint8_t* v8, const float* m_scale, 
 
 int sl_embed_lookup(const int32_t* ids, const void* T_S, const void* T_perp, const void* pos, int table_type, float scale,
                     uint64_t n_tok, uint32_t L, uint64_t V, uint32_t d, void* X, int x_type, uint32_t* flags, void* stream) {
-  if (!ids || !T_S || !X || !type_ok(table_type) || !type_ok(x_type) || d < 1 || V < 1 || (pos && L < 1) || !std::isfinite(scale))
+  if (!T_S || (n_tok > 0 && (!ids || !X)) || !type_ok(table_type) || !type_ok(x_type) || d < 1 || V < 1 || (pos && L < 1) || !std::isfinite(scale))
     return SL_ERR_INVALID_ARG;
   if (!is_aligned(ids, 4) || !typed_aligned(T_S, table_type) || !typed_aligned(T_perp, table_type) || !typed_aligned(pos, table_type) ||
       !typed_aligned(X, x_type) || !is_aligned(flags, 4))
@@ -250,7 +251,9 @@ int sl_norm_block(const void* x, const void* b, const void* g, int res_type, int
                   float* r_post, float* r_pre, uint32_t* flags, void* stream) {
   int rc = norm_types_check(res_type, act_type, w_type);
   if (rc != SL_OK) return rc;
-  if (!x || d < 1 || !std::isfinite(alpha) || !(eps >= 0) || !std::isfinite(eps)) return SL_ERR_INVALID_ARG;
+  if (d < 1 || !std::isfinite(alpha) || !(eps >= 0) || !std::isfinite(eps)) return SL_ERR_INVALID_ARG;
+  if (n == 0) return d > SL_MAX_WIDTH ? SL_ERR_UNSUPPORTED : SL_OK;        // no pointer tells what is there: empty arrays may have none
+  if (!x) return SL_ERR_INVALID_ARG;
   if (b ? (!h || ldb < d || (g && ldg < d)) : (g || w_post || h || !y)) return SL_ERR_INVALID_ARG;
   if ((y && !w_pre) || (!y && (w_pre || r_pre))) return SL_ERR_INVALID_ARG;
   if (!typed_aligned(x, res_type) || !typed_aligned(h, res_type) || !typed_aligned(b, act_type) || !typed_aligned(g, act_type) ||
@@ -258,7 +261,6 @@ int sl_norm_block(const void* x, const void* b, const void* g, int res_type, int
       !is_aligned(r_pre, 4) || !is_aligned(flags, 4))
     return SL_ERR_ALIGNMENT;
   if (n > 0x7FFFFFFFull || d > SL_MAX_WIDTH) return SL_ERR_UNSUPPORTED;
-  if (n == 0) return SL_OK;
   NormArgs a{x, b, g, w_post, w_pre, h, y, r_post, r_pre, b ? ldb : 0, g ? ldg : 0, (uint32_t)n, d, alpha, eps, w_type == SL_BF16, flags,
              debug_wait_polls()};
   return status(launch_norm_block(a, res_type, act_type, (cudaStream_t)stream));
@@ -273,12 +275,14 @@ int sl_norm_block_grad(const void* dh, const void* dy, const void* h, const void
   int rc = norm_types_check(res_type, act_type, w_type);
   if (rc != SL_OK) return rc;
   if (d < 1 || !std::isfinite(alpha)) return SL_ERR_INVALID_ARG;
-  if (n > 0 && (!h || !dx || (!dh && !dy))) return SL_ERR_INVALID_ARG;
-  if (b ? (!db || ldb < d || (g && ldg < d)) : (g || w_post || db)) return SL_ERR_INVALID_ARG;
-  if ((g != nullptr) != (dg != nullptr) || (w_post && !r_post) || (w_post != nullptr) != (dw_post != nullptr)) return SL_ERR_INVALID_ARG;
-  if ((dy != nullptr) != (w_pre != nullptr) || (dy != nullptr) != (r_pre != nullptr) || (dy != nullptr) != (dw_pre != nullptr))
-    return SL_ERR_INVALID_ARG;
-  if (n > 0 && (dw_post || dw_pre) && !ws) return SL_ERR_INVALID_ARG;
+  if (n > 0) {                                             // of no rows only the weights' gradients (zeros) are looked at
+    if (!h || !dx || (!dh && !dy)) return SL_ERR_INVALID_ARG;
+    if (b ? (!db || ldb < d || (g && ldg < d)) : (g || w_post || db)) return SL_ERR_INVALID_ARG;
+    if ((g != nullptr) != (dg != nullptr) || (w_post && !r_post) || (w_post != nullptr) != (dw_post != nullptr)) return SL_ERR_INVALID_ARG;
+    if ((dy != nullptr) != (w_pre != nullptr) || (dy != nullptr) != (r_pre != nullptr) || (dy != nullptr) != (dw_pre != nullptr))
+      return SL_ERR_INVALID_ARG;
+    if ((dw_post || dw_pre) && !ws) return SL_ERR_INVALID_ARG;
+  }
   if (!typed_aligned(dh, res_type) || !typed_aligned(h, res_type) || !typed_aligned(dx, res_type) || !typed_aligned(dy, act_type) ||
       !typed_aligned(b, act_type) || !typed_aligned(g, act_type) || !typed_aligned(db, act_type) || !typed_aligned(dg, act_type) ||
       !typed_aligned(w_post, w_type) || !typed_aligned(w_pre, w_type) || !typed_aligned(dw_post, w_type) ||

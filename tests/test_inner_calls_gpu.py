@@ -178,3 +178,24 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     for call in calls:
         with pytest.raises(ValueError, match="current CUDA device"):
             call()
+
+
+def test_no_tokens_and_no_elements():
+    d, V, L = 24, 10, 4
+    T, P, w = _randn(V, d).requires_grad_(), _randn(L, d, seed=1).requires_grad_(), _randn(d, seed=2).requires_grad_()
+    ids = torch.zeros(0, 5, dtype=torch.int32, device="cuda")
+    x = inner.embed_lookup(ids, T, T, P)
+    assert x.shape == (0, 5, d)
+    b = torch.zeros(0, 5, d, device="cuda", requires_grad=True)
+    for form in ((x, b, b, w, w), (x, b, None, None, w), (x, b, None, w, None), (x, None, None, None, w)):
+        h, y = inner.norm_block(*form)
+        assert all(t is None or t.shape == x.shape for t in (h, y))
+        loss = sum(t.sum() for t in (h, y) if t is not None)
+        used = [T, P] + [t for t in (b, w) if any(t is u for u in form)]
+        for t, g in zip(used, torch.autograd.grad(loss, used, retain_graph=True)):
+            assert g.shape == t.shape and not g.any()
+    for bits in (8, 32):
+        opt = inner.AdamW(torch.zeros(0, device="cuda"), [0, 0], bits=bits)
+        opt.step(torch.zeros(0, device="cuda"))
+        assert opt.steps == 1 and all(t.numel() == 0 for t in opt.moments())
+        opt.load_moments(*opt.moments(), 5)

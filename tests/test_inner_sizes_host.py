@@ -31,3 +31,19 @@ def test_widths_that_no_grid_holds_are_refused(lib):
     UNS = api.SL_ERR_UNSUPPORTED
     assert call(65535 * 64 + 1) == UNS and call(65535 * 64 + 8, dX=P + 4) == UNS      # single elements: 64 columns to a CTA
     assert call(65535 * 128 + 8) == UNS and call(1 << 31) == UNS                      # vectors: 128
+
+
+def test_empty_arrays_may_have_no_memory(lib):
+    lay, OK = api.Layout([0, 0]).ref(), api.SL_OK
+    hyper = (0, 1e-3, 0.9, 0.95, 1e-8, 1, 0, 0, 0)
+    assert lib.sl_adamw(0, 0, 0, 0, 0, 0, 0, lay, *hyper) == OK and lib.sl_adamw8(0, 0, 0, 0, 0, 0, 0, 0, 0, lay, *hyper) == OK
+    assert lib.sl_adamw8_pack(0, 0, lay, 0, 0, 0, 0, 0) == OK and lib.sl_adamw8_unpack(0, 0, 0, 0, lay, 0, 0, 0) == OK
+    assert lib.sl_embed_lookup(0, P, P, P, 0, 1.0, 0, 2, 10, 8, 0, 0, 0, 0) == OK
+    assert lib.sl_norm_block(0, 0, 0, 0, 0, P, P, 0, 0, 8, 8, 8, 1.0, 1e-6, 0, 0, 0, 0, 0, 0) == OK
+    assert lib.sl_norm_block_grad(0, 0, 0, 0, 0, 0, 0, P, P, 0, 0, 0, 0, 8, 8, 8, 1.0, 0, 0, 0, 0, 0, 1, 0, 0, 0) == OK
+    # what does not depend on their number is still checked
+    INV = api.SL_ERR_INVALID_ARG
+    assert lib.sl_embed_lookup(0, 0, P, P, 0, 1.0, 0, 2, 10, 8, 0, 0, 0, 0) == INV
+    assert lib.sl_embed_lookup(0, P, P, P, 0, float("nan"), 0, 2, 10, 8, 0, 0, 0, 0) == INV
+    assert lib.sl_norm_block(0, 0, 0, 0, 0, P, P, 0, 0, 0, 8, 8, 1.0, 1e-6, 0, 0, 0, 0, 0, 0) == INV
+    assert lib.sl_adamw(0, 0, 0, 0, 0, 0, 0, lay, 0, -1.0, 0.9, 0.95, 1e-8, 1, 0, 0, 0) == INV
