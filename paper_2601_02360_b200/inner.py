@@ -174,11 +174,11 @@ class AdamW:
         """One step from the gradient arena `grad`; `grad_scale` (a device scalar, float32) multiplies it first: a clipping
         coefficient costs no synchronisation.  If it is not finite the device skips the step and raises SL_FLAG_NONFINITE
         in `flags`; the step count goes on."""
-        self.steps += 1
         call = api.sl_adamw8 if self.bits == 8 else api.sl_adamw
         with torch.cuda.device_of(self.theta):
-            call(self.theta, grad, *self.states, self.layout, self.lr, *self.betas, self.eps, self.steps, decay=self.decay,
+            call(self.theta, grad, *self.states, self.layout, self.lr, *self.betas, self.eps, self.steps + 1, decay=self.decay,
                  grad_scale=grad_scale, copy=self.copy, flags=self.flags, stream=stream)
+        self.steps += 1                                   # a step that was refused does not count
 
     def moments(self):
         """(m, v) as float32: the moments themselves, or the values that their codes stand for."""

@@ -199,3 +199,18 @@ def test_no_tokens_and_no_elements():
         opt.step(torch.zeros(0, device="cuda"))
         assert opt.steps == 1 and all(t.numel() == 0 for t in opt.moments())
         opt.load_moments(*opt.moments(), 5)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_step_that_is_refused_does_not_count(bits):
+    n = 600
+    th, g = _randn(n), _randn(n, seed=1)
+    one, two = (inner.AdamW(th.clone(), [0, n], bits=bits) for _ in range(2))
+    for bad in (g[:-1], g.cpu(), g.double()):
+        with pytest.raises(ValueError):
+            one.step(bad)
+    assert one.steps == 0
+    for _ in range(2):
+        one.step(g)
+        two.step(g)
+    assert one.steps == 2 and torch.equal(one.theta, two.theta)
