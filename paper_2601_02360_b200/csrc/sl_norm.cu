@@ -503,8 +503,9 @@ __global__ void __maxnreg__(128) norm_block_grad_kernel(const NormGradArgs a, co
       }
     }
     row_sum(s, l.width);
-    const float ch = rh * rh * rh * inv_d * s[0];                    // dx = z - ch h
-    const float cb = rp * rp * inv_d * (s[1] - ch * s[2]);          // db = rp (q - cb b)
+    // rms(h)^3 alone leaves float32 where rms(h)^2 and the products with the sums do not
+    const float ch = rh * ((rh * inv_d) * (rh * s[0]));              // dx = z - ch h
+    const float cb = rp * (inv_d * (rp * (s[1] - ch * s[2])));      // db = rp (q - cb b)
     h.forget();
     if (a.b) b.forget();
     if (a.g) g.forget();
