@@ -86,6 +86,17 @@ struct Piece {
   }
 };
 
+// elements of a k-th piece that are not the row's, as mask() does, for a value that several arrays enter
+template <int E, int K, bool SHIFT>
+__device__ __forceinline__ void zero_outside(const Columns<E, K, SHIFT>& c, int k, float (&f)[E]) {
+  if constexpr (SHIFT)
+    if (!c.whole(k)) {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (!c.has(k, e)) f[e] = 0.0f;
+    }
+}
+
 template <class T, int E, int K, bool SHIFT>
 __device__ __forceinline__ void store_part(T* row, const Columns<E, K, SHIFT>& c, int k, const float (&f)[E]) {
   T* p = row + c.col(k);
@@ -305,6 +316,7 @@ struct Launch {
   int width;
   uint32_t period;
   uint32_t busy;                   // groups that have a row: the first ones
+  uint32_t near;                   // rows_near_end()
 };
 template <Group G>
 struct Rows {
@@ -332,7 +344,7 @@ __global__ void __launch_bounds__(kMaxThreads) norm_block_kernel(const NormArgs 
   Piece<AT, E, K> b, g;
   auto load = [&](uint64_t r) {
     if (r >= a.n) return;
-    const bool near_end = SHIFT && near_array_end(r, a.n, a.d);
+    const bool near_end = SHIFT && near_array_end(r, a.n, l.near);
     x.load(static_cast<const RT*>(a.x) + r * a.d, c, near_end);
     if (a.b) b.load(static_cast<const AT*>(a.b) + r * a.ldb, c, near_end);
     if (a.g) g.load(static_cast<const AT*>(a.g) + r * a.ldg, c, near_end);
@@ -348,9 +360,7 @@ __global__ void __launch_bounds__(kMaxThreads) norm_block_kernel(const NormArgs 
   group_barrier<G>();
   for (; rw.base < a.n; rw.base += rw.step, r += rw.step) {
     const bool in = r < a.n;
-    x.mask(c);
-    if (a.b) b.mask(c);
-    if (a.g) g.mask(c);                                    // a NaN beside the row would outlast the zeros of x and b
+    if (a.w_post) b.mask(c);
     float h[K][E];
     float rp = a.alpha;                                    // factor of u: rms(b), with alpha in w_post, or alpha
     if (a.w_post) {
@@ -383,6 +393,7 @@ __global__ void __launch_bounds__(kMaxThreads) norm_block_kernel(const NormArgs 
 #pragma unroll
         for (int e = 0; e < E; ++e) h[k][e] = __fmaf_rn(rp, u[e], h[k][e]);
       }
+      if (a.y) zero_outside(c, k, h[k]);                   // x and g beside the row may hold anything, NaN too
     }
     load(r + rw.step);                                     // the next row is on its way while this one is finished
     if (a.b && in) {
@@ -436,7 +447,7 @@ __global__ void __maxnreg__(128) norm_block_grad_kernel(const NormGradArgs a, co
   float rh = 0.0f, rp = 1.0f;
   auto load = [&](uint64_t r) {
     if (r >= a.n) return;
-    const bool near_end = SHIFT && near_array_end(r, a.n, a.d);
+    const bool near_end = SHIFT && near_array_end(r, a.n, l.near);
     h.load(static_cast<const RT*>(a.h) + r * a.d, c, near_end);
     if (a.dh) dh.load(static_cast<const RT*>(a.dh) + r * a.d, c, near_end);
     if (a.dy) {
@@ -462,8 +473,6 @@ __global__ void __maxnreg__(128) norm_block_grad_kernel(const NormGradArgs a, co
     h.mask(c);
     if (a.dh) dh.mask(c);
     if (a.dy) dy.mask(c);
-    if (a.b) b.mask(c);
-    if (a.g) g.mask(c);
     float z[K][E];
     float s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -494,6 +503,7 @@ __global__ void __maxnreg__(128) norm_block_grad_kernel(const NormGradArgs a, co
           if (a.g)
 #pragma unroll
             for (int e = 0; e < E; ++e) w[e] = w[e] * sigmoid(g.get(k, e));
+          zero_outside(c, k, w);                           // b and g beside the row may hold anything, NaN too
 #pragma unroll
           for (int e = 0; e < E; ++e) {
             s[1] = __fmaf_rn(w[e], z[k][e], s[1]);
@@ -650,6 +660,7 @@ inline Shape shape_of(uint32_t d, bool aligned, const uint64_t* places, int n, u
   s.vec = aligned ? 8 : 1;
   s.shift = aligned && d % 8 != 0;
   s.l.period = 1;
+  s.l.near = rows_near_end(d);
   if (s.shift)
     while ((uint64_t)s.l.period * d % 8 != 0) s.l.period *= 2;
   const uint32_t parts = s.vec == 8 ? (d + (s.shift ? 7 : 0) + 7) / 8 : d, per_thread = s.vec == 8 ? 2 : 16;

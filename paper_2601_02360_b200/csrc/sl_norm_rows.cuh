@@ -31,8 +31,9 @@ __host__ __device__ __forceinline__ Columns<E, K, SHIFT> columns_of(uint64_t row
   return c;
 }
 
-// A vector with the end of a row reaches up to 7 elements past it: fewer than 7 come behind this row.  That is the last row
-// alone from d = 7 on, and up to seven rows below.  (Rows that lie further apart leave more room.)
-__host__ __device__ __forceinline__ bool near_array_end(uint64_t row, uint32_t n, uint32_t d) { return (n - 1 - row) * d < 7; }
+// A vector with the end of a row reaches up to 7 elements past it; so many rows from the last one on have fewer than 7 behind them
+// (one from d = 7 on, up to seven below; rows that lie further apart leave more room).
+__host__ __device__ __forceinline__ uint32_t rows_near_end(uint32_t d) { return 6 / d + 1; }
+__host__ __device__ __forceinline__ bool near_array_end(uint64_t row, uint32_t n, uint32_t near) { return row + near >= n; }
 
 }  // namespace sl

@@ -14,7 +14,7 @@ int main() {
           for (uint64_t r = 0; r < n; ++r)
             for (uint32_t lane = 0; lane < lanes; ++lane) {
               const auto c = sl::columns_of<8, 2, true>(r, lane, lanes, d);
-              const bool near_end = sl::near_array_end(r, n, d);
+              const bool near_end = sl::near_array_end(r, n, sl::rows_near_end(d));
               const int64_t end = (int64_t)(n - 1) * (d + gap) + d;
               for (int k = 0; k < 2; ++k)
                 for (int e = 0; e < 8; ++e) {
