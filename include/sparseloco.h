@@ -324,8 +324,8 @@ int sl_embed_lookup(const int32_t* ids, const void* T_S, const void* T_perp, con
  *     dpos[l,:] (+)= sum over t with t mod L = l of dX[t,:]              L x d; NULL: not computed
  * Sums are float32 in an order fixed by ids, n_tok and d alone (tokens ascending inside each part of a sum),
  * so results are reproducible bit for bit; no float atomics.  dX is n_tok x d of dx_type, dT and dpos
- * are of dt_type.  Ids outside [0, V) contribute nothing and raise SL_FLAG_BAD_INDEX.  Rows without a
- * token: zeros with acc = 0, untouched with acc = 1.
+ * are of dt_type.  Ids outside [0, V) contribute nothing and raise SL_FLAG_BAD_INDEX.  Rows of dT and dpos
+ * without a token: zeros with acc = 0, untouched with acc = 1.
  * ws: DEVICE workspace of sl_embed_grad_workspace(n_tok, V, d) bytes (0 for sizes that are refused), 32-byte aligned; its
  * contents before and after the call do not matter.  n_tok, V < 2^31; widths above 65535 * 64 may be SL_ERR_UNSUPPORTED. */
 uint64_t sl_embed_grad_workspace(uint64_t n_tok, uint64_t V, uint32_t d);

@@ -477,6 +477,7 @@ __device__ void sum_positions(const EmbedGradArgs& a, const PosArgs& q, uint64_t
     for (int i = 0; i < PER; ++i) c[i] = c0 + i * q.tx * E < a.d ? c0 + i * q.tx * E : 0;
     const uint32_t rows = l < a.n_tok ? (a.n_tok - l + a.L - 1) / a.L : 0;        // tokens at this position
     const uint32_t lo = min(cut * q.per_cut, rows), hi = min(lo + q.per_cut, rows);
+    if (a.acc && rows == 0) continue;                // nothing to add
     float sum[PER][E] = {}, old[PER][E] = {};
     DT* out = static_cast<DT*>(a.dpos) + (uint64_t)l * a.d;
     if (!q.part && a.acc)
