@@ -178,6 +178,10 @@ class AdamW:
         with torch.cuda.device_of(self.theta):
             call(self.theta, grad, *self.states, self.layout, self.lr, *self.betas, self.eps, self.steps + 1, decay=self.decay,
                  grad_scale=grad_scale, copy=self.copy, flags=self.flags, stream=stream)
+        # as torch's in-place operations do: a graph that saved these parameters may not be used with the new ones
+        torch.autograd.graph.increment_version(self.theta)
+        if self.copy is not None:
+            torch.autograd.graph.increment_version(self.copy)
         self.steps += 1                                   # a step that was refused does not count
 
     def moments(self):

@@ -214,3 +214,18 @@ def test_a_step_that_is_refused_does_not_count(bits):
         one.step(g)
         two.step(g)
     assert one.steps == 2 and torch.equal(one.theta, two.theta)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_graph_of_the_old_parameters_is_refused_after_a_step(bits):
+    d = 24
+    theta, copy = torch.ones(d, device="cuda"), torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    opt = inner.AdamW(theta, [0, d], bits=bits, copy=copy)
+    x = _randn(5, d)
+    for w in (theta, copy):
+        p = w.detach().requires_grad_()
+        _, y = inner.norm_block(x, w_pre=p)
+        y.sum().backward(retain_graph=True)
+        opt.step(torch.ones(d, device="cuda"))
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
