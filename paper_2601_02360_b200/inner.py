@@ -195,6 +195,9 @@ class AdamW:
 
     def load_moments(self, m: torch.Tensor, v: torch.Tensor, steps: int) -> None:
         """Takes over float32 moments (of either form: an optimiser can change its form between two steps)."""
+        for name, t in (("m", m), ("v", v)):
+            if t.numel() != self.layout.n_total:
+                raise ValueError(f"{name}: expected {self.layout.n_total} elements, got {list(t.shape)}")
         if self.bits == 32:
             self.states[0].copy_(m)
             self.states[1].copy_(v)

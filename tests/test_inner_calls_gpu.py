@@ -229,3 +229,16 @@ def test_a_graph_of_the_old_parameters_is_refused_after_a_step(bits):
         opt.step(torch.ones(d, device="cuda"))
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             y.sum().backward()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_moments_of_another_size_are_refused(bits):
+    n = 600
+    opt = inner.AdamW(torch.zeros(n, device="cuda"), [0, n], bits=bits)
+    opt.load_moments(_randn(n), _randn(n, seed=1).abs(), 7)
+    before = [t.clone() for t in opt.states]
+    for bad in (_randn(1), _randn(n + 1), _randn(n - 1)):
+        for m, v in ((bad, _randn(n)), (_randn(n), bad.abs())):
+            with pytest.raises(ValueError):
+                opt.load_moments(m, v, 9)
+    assert opt.steps == 7 and all(torch.equal(a, b) for a, b in zip(before, opt.states))
