@@ -254,7 +254,8 @@ int sl_round_tf32(float* x, uint64_t n, void* stream);
  * tables.  Element types are arguments here because parameters, gradients and activations combine
  * freely: SL_F32 is float, SL_BF16 the upper half of one (uint16_t).  Arithmetic is float32 whatever the
  * storage; storing to bfloat16 rounds once, to nearest even.  float arrays that start on 32 bytes and
- * bfloat16 ones that start on 16 are moved in vectors; any other start gives the same results more slowly.
+ * bfloat16 ones that start on 16 are moved in vectors; any other start is slower.  AdamW and the lookup
+ * give the same bits there; where values are summed (norms, gradients) the order of a sum may be another.
  * No tokens, rows or elements at all: arrays that would be empty may be NULL, and nothing is written but the zeros of sums over
  * nothing.
  * ------------------------------------------------------------------------------------------------ */
@@ -322,8 +323,8 @@ int sl_embed_lookup(const int32_t* ids, const void* T_S, const void* T_perp, con
 /* Gradient of the lookup.  With acc = 0 the outputs are overwritten, with acc = 1 they are added to:
  *     dT[v,:]   (+)= scale * sum over t with ids[t] = v of dX[t,:]       V x d; the gradient of T_S, and of T_perp
  *     dpos[l,:] (+)= sum over t with t mod L = l of dX[t,:]              L x d; NULL: not computed
- * Sums are float32 in an order fixed by ids, n_tok and d alone (tokens ascending inside each part of a sum),
- * so results are reproducible bit for bit; no float atomics.  dX is n_tok x d of dx_type, dT and dpos
+ * Sums are float32 in an order fixed by ids, n_tok, L and d and by whether the arrays start where vectors may
+ * (tokens ascending inside each part of a sum), so equal calls give equal bits; no float atomics.  dX is n_tok x d of dx_type, dT and dpos
  * are of dt_type.  Ids outside [0, V) contribute nothing and raise SL_FLAG_BAD_INDEX.  Rows of dT and dpos
  * without a token: zeros with acc = 0, untouched with acc = 1.
  * ws: DEVICE workspace of sl_embed_grad_workspace(n_tok, V, d) bytes (0 for sizes that are refused), 32-byte aligned; its
@@ -345,7 +346,10 @@ int sl_embed_grad(const int32_t* ids, const void* dX, int dx_type, float scale, 
  * Left out when NULL: g (no gate), w_post (no norm after the block), y with w_pre (no norm follows), b
  * with g, w_post and h (the norm before the first block: y = x * rms(x) * w_pre).
  * y is formed from the float32 h, before h is rounded to res_type.  d <= SL_MAX_WIDTH, n < 2^31.
- * flags: optional; SL_FLAG_TIMEOUT if a wait inside a row's group of CTAs (d > 2048) gave up. */
+ * sigmoid comes from a fast exponential and reciprocal: its relative error is at most (8 + 1.3 |g|) 2^-24, and below 2^-126
+ * it is 0.
+ * flags: optional; SL_FLAG_TIMEOUT if a wait inside a row's group of CTAs gave up, after which the outputs are not to be used.
+ * Rows of up to 2560 elements have one CTA and no such wait; wider ones may have several. */
 #define SL_MAX_WIDTH 16384
 int sl_norm_block(const void* x, const void* b, const void* g, int res_type, int act_type, const void* w_post,
                   const void* w_pre, int w_type, uint64_t n, uint32_t d, uint64_t ldb, uint64_t ldg, float alpha, float eps,
@@ -359,7 +363,8 @@ int sl_norm_block(const void* x, const void* b, const void* g, int res_type, int
  * h, b, g, w_post, w_pre, r_post, r_pre: as given to and written by sl_norm_block (h is x when b is
  * NULL).  g and dg, w_post with r_post and dw_post, and (with dy) w_pre, r_pre and dw_pre go together
  * (r_post is not looked at without w_post).
- * Row sums are float32; weight gradients are sums over rows in an order fixed by n and d.
+ * Row sums are float32; weight gradients are sums over rows, cut by how many rows the device holds at once: in an order fixed by
+ * n, d, the types, the row distances, whether arrays start where vectors may, and the device.
  * ws: DEVICE workspace of sl_norm_block_grad_workspace(n, d) bytes, 16-byte aligned. */
 uint64_t sl_norm_block_grad_workspace(uint64_t n, uint32_t d);
 int sl_norm_block_grad(const void* dh, const void* dy, const void* h, const void* b, const void* g, int res_type,

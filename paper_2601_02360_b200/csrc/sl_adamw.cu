@@ -16,7 +16,7 @@ struct Seg {
 };
 
 // Walks the blocks of an arena in ascending order; the tensor of the last one is kept in registers.
-// SHIFT: blocks begin on a grid; the 8-bit form's begin at their tensor (634 -> 596 us for 187 M elements without the shift)
+// SHIFT: blocks begin on a grid; the 8-bit form's begin at their tensor (634 -> 598 us for 187 M elements without the shift)
 template <int T, bool SHIFT>
 struct Walk {
   const BlockTable<T>& tb;
@@ -82,7 +82,7 @@ __device__ __forceinline__ void adamw_element(const AdamwHyper& h, float keep, f
 
 // Whether FAST keeps its bound: a flushed v < 2^-126 takes less than 2^-63 a from denom, at most 2^-22 of it from this eps on
 // (1.4e-11 for a = 31.6, the first step at beta2 = 0.999; below, an eps that is subnormal itself would even give 0 * inf where
-// v = 0); and 1 / denom must not be subnormal.
+// v = 0); and 1 / denom must not be subnormal.  The exact form takes 700 us for the 187 M elements that take 587.
 inline bool fast_move(const AdamwHyper& h) { return h.eps >= h.a * 0x1p-41f && h.eps <= 0x1p100f; }
 
 // the gradient's factor; false (with the flag raised): skip the step

@@ -81,7 +81,7 @@ def embed_lookup(ids, T_S, T_perp=None, pos=None, scale: float = 1.0, flags=None
     """scale (T_S[ids] + T_perp[ids]) + pos[t mod L] for int32 ids of any shape, [..., d]; token t is the t-th of the
     flattened ids, L the rows of pos.  Differentiable in T_S, T_perp and pos; a second derivative raises RuntimeError."""
     if T_S.dim() != 2 or (T_perp is not None and T_perp.shape != T_S.shape):
-        raise ValueError(f"T_S, T_perp: expected two matrices of one shape, got {list(T_S.shape)} and {None if T_perp is None else list(T_perp.shape)}")
+        raise ValueError(f"T_S, T_perp: expected matrices of one shape, got {[list(t.shape) for t in (T_S, T_perp) if t is not None]}")
     if pos is not None and (pos.dim() != 2 or pos.shape[0] < 1 or pos.shape[1] != T_S.shape[1]):
         raise ValueError(f"pos: expected rows of {T_S.shape[1]}, got {list(pos.shape)}")
     L = pos.shape[0] if pos is not None else 1
