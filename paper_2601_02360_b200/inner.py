@@ -18,8 +18,16 @@ import torch
 from . import api
 
 
-def _dense(t):
-    return None if t is None else t.resolve_neg().contiguous()
+def _dense(t, *shape):
+    """t without gaps (in another shape, if one is given); what is not needed is not done: on a tensor of a graph each operation
+    costs a node, and 4 us a call."""
+    if t is None:
+        return None
+    if shape and t.shape != shape:
+        t = t.reshape(shape)
+    if t.is_neg():
+        t = t.resolve_neg()
+    return t if t.is_contiguous() else t.contiguous()
 
 
 class _Once(torch.autograd.Function):
@@ -50,7 +58,7 @@ def _once_differentiable(backward):
 
 
 class _EmbedLookup(torch.autograd.Function):
-    """Dense arguments: ids [n], tables [V, d], positions [L, d]."""
+    """Dense arguments: ids in any shape, tables [V, d], positions [L, d]."""
 
     @staticmethod
     def forward(ctx, ids, T_S, T_perp, pos, L, scale, flags, out_dtype):
@@ -61,7 +69,7 @@ class _EmbedLookup(torch.autograd.Function):
             api.sl_embed_lookup(ids, T_S, T_perp, pos, scale, n, L, V, d, X, flags)
         ctx.save_for_backward(ids)
         ctx.sizes = (n, L, V, d, scale, T_S.dtype, flags)
-        return X
+        return X.view(*ids.shape, d)
 
     @staticmethod
     @_once_differentiable
@@ -85,8 +93,7 @@ def embed_lookup(ids, T_S, T_perp=None, pos=None, scale: float = 1.0, flags=None
     if pos is not None and (pos.dim() != 2 or pos.shape[0] < 1 or pos.shape[1] != T_S.shape[1]):
         raise ValueError(f"pos: expected rows of {T_S.shape[1]}, got {list(pos.shape)}")
     L = pos.shape[0] if pos is not None else 1
-    X = _EmbedLookup.apply(_dense(ids.reshape(-1)), _dense(T_S), _dense(T_perp), _dense(pos), L, float(scale), flags, out_dtype)
-    return X.view(*ids.shape, T_S.shape[1])
+    return _EmbedLookup.apply(_dense(ids), _dense(T_S), _dense(T_perp), _dense(pos), L, float(scale), flags, out_dtype)
 
 
 class _NormBlock(torch.autograd.Function):
@@ -135,8 +142,14 @@ def _rows(name: str, t, n: int, d: int):
         return None
     if t.shape[-1:] != (d,) or t.numel() != n * d:
         raise ValueError(f"{name}: expected {n} rows of {d}, got {list(t.shape)}")
-    v = t.resolve_neg().reshape(n, d)
-    return v if v.stride(1) == 1 and (n <= 1 or v.stride(0) >= d) else v.contiguous()
+    v = t if t.dim() == 2 else t.reshape(n, d)
+    return v if v.stride(1) == 1 and (n <= 1 or v.stride(0) >= d) and not v.is_neg() else _dense(v)
+
+
+def _weight(name: str, w, d: int):
+    if w is not None and (w.shape[-1:] != (d,) or w.numel() != d):
+        raise ValueError(f"{name}: expected {d} elements, got {list(w.shape)}")
+    return _dense(w, d)
 
 
 def norm_block(x, b=None, g=None, w_post=None, w_pre=None, alpha: float = 1.0, eps: float = 1e-6, flags=None):
@@ -148,9 +161,10 @@ def norm_block(x, b=None, g=None, w_post=None, w_pre=None, alpha: float = 1.0, e
     if d < 1:
         raise ValueError(f"x: expected rows, got {list(x.shape)}")
     n = x.numel() // d
-    weight = lambda name, w: None if w is None else _rows(name, w, 1, d).reshape(d)  # noqa: E731
-    h, y = _NormBlock.apply(_dense(x.reshape(n, d)), _rows("b", b, n, d), _rows("g", g, n, d), weight("w_post", w_post),
-                            weight("w_pre", w_pre), float(alpha), float(eps), flags)
+    h, y = _NormBlock.apply(_dense(x, n, d), _rows("b", b, n, d), _rows("g", g, n, d), _weight("w_post", w_post, d),
+                            _weight("w_pre", w_pre, d), float(alpha), float(eps), flags)
+    if x.dim() == 2:
+        return h, y
     return (None if h is None else h.view(x.shape)), (None if y is None else y.view(x.shape))
 
 
